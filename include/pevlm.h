@@ -311,6 +311,88 @@ pevlm_status pevlm_block_prefill_attn_fp8(const void *q, const void *k, const vo
                                           const pevlm_layout *layout, const pevlm_heads *heads, void *workspace,
                                           size_t workspace_bytes, int32_t stages, void *stream);
 
+/* ---- paged KV cache in 4 bits: from the prompt's prefill to the last token of the answer
+ *
+ * A request's tokens lie in pages of page_size tokens of a pool that all requests share; column c of row s of
+ * block_table names the page of tokens c * page_size .. of request s.  The SLOT of a token is its place in the pool,
+ * page * page_size + (token % page_size).
+ *
+ * Pool (DEVICE, 16-byte aligned, pevlm_cache_pool_bytes): [num_pages][Hkv][page_size / 16] records of 17 * head_dim bytes.  A record holds
+ * 16 neighbouring tokens of one KV head:
+ *   K codes  [head_dim / 32][16 tokens][16 bytes]   block b of 32 elements, byte j: elements 2j (low half) and 2j + 1
+ *   V codes  the same
+ *   scales   [head_dim / 32][16 tokens][2]          scale bytes of K and of V
+ * A block is 32 neighbouring elements of a token: 4-bit codes (E2M1: sign, two exponent bits with bias 1, one mantissa bit;
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6) times 2^(s - 127), s its scale byte.  The exponent is the smallest with amax <= 6 * 2^e (amax: the
+ * block's largest magnitude; e = 0 if that is 0), within [-100, 125]; codes are rounded to nearest, ties to even, and saturate.
+ * A block that holds an infinity or a NaN is kept as s = 255, which stands for NaN in all of its elements.  4.25 bits an element.
+ *
+ * Lengths, tables, slots and row ranges are DEVICE int32 arrays that the kernels read on `stream`: no call needs them on the host, and
+ * a step of generation can be captured into a graph once and replayed while they change.  What they hold is bounded, not
+ * trusted: nothing outside the pool, the table or the rows is read or written, whatever they say.  The arrays of a call do
+ * not overlap unless it says so. */
+typedef struct {
+    void *pool;                 /* DEVICE */
+    int32_t num_pages;          /* >= 1; num_pages * page_size below 2^31 */
+    int32_t page_size;          /* tokens of a page: a power of two from 16 to 4096 */
+    int32_t num_seqs;           /* >= 1 requests */
+    int32_t max_pages;          /* >= 1 columns of the table; max_pages * page_size below 2^31 */
+    int32_t *block_table;       /* DEVICE [num_seqs][max_pages] */
+} pevlm_cache;
+
+/* Bytes of a pool (0 for an invalid descriptor). */
+size_t pevlm_cache_pool_bytes(const pevlm_heads *heads, int32_t num_pages, int32_t page_size);
+
+/*
+ * Pages, slots and positions of new tokens, from the requests' lengths.  Request s holds seq_len[s] tokens and gets new_len[s]
+ * more (NULL: one each; negative entries count as 0), which are rows row_start[s] .. of the packed q, k and v of this step, requests one
+ * after another.  Pages that it then lacks come from the end of the list free_pages[0 .. num_free[0]), an array of free_capacity entries.
+ *   seq_len_out [num_seqs]     tokens held afterwards (may be seq_len itself)
+ *   num_free_out [1]           pages left in the list (may be num_free itself)
+ *   row_start, row_len [num_seqs]  the request's rows; row_len is 0 for a request that is not served
+ *   slot_map [num_rows]        slot of every row; -1 for rows of no request, of one that is not served, or on a page outside the pool
+ *   pos_ids [3][num_rows]      the token's index in its request plus pos_offset[s] (NULL: 0), three times, as
+ *                              pevlm_rope_mrope takes it; 0 for rows without a token; NULL: not wanted
+ *   block_table                gets the new pages; other entries stay as they are
+ * A request is not served, and keeps what it has, if it would outgrow its row of the table, if its rows end behind num_rows, or
+ * if the list does not hold the pages that it and those of the requests before it need that fit otherwise.
+ * num_free is taken within [0, free_capacity], seq_len from 0 on.  Workspace: pevlm_cache_slots_workspace_bytes.
+ */
+size_t pevlm_cache_slots_workspace_bytes(int32_t num_seqs);
+pevlm_status pevlm_cache_slots(const pevlm_cache *cache, const int32_t *seq_len, const int32_t *new_len, const int32_t *free_pages,
+                               int32_t free_capacity, const int32_t *num_free, int32_t num_rows, const int32_t *pos_offset, int32_t *seq_len_out,
+                               int32_t *num_free_out, int32_t *row_start, int32_t *row_len, int32_t *slot_map, int32_t *pos_ids,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * K and V of num_rows tokens into the slots slot_map names (rows whose slot is outside the pool, as -1 is, go nowhere; the slots of
+ * a call are distinct), and the values of such slots back (rows without a slot are left as they were).  Rows of k and v are [Hkv][D]
+ * of heads->dtype, k_stride and v_stride elements apart (0: contiguous; otherwise at least Hkv * D and a multiple of 8), bases 16-byte
+ * aligned.  K is kept as given, so it is rotated first.  Of heads only n_kv_heads, head_dim and dtype matter.  block_table may be NULL.
+ */
+pevlm_status pevlm_cache_store_kv4(const void *k, const void *v, int64_t k_stride, int64_t v_stride, const int32_t *slot_map, int32_t num_rows,
+                                   const pevlm_cache *cache, const pevlm_heads *heads, void *stream);
+pevlm_status pevlm_cache_load_kv4(void *k, void *v, int64_t k_stride, int64_t v_stride, const int32_t *slot_map, int32_t num_rows,
+                                  const pevlm_cache *cache, const pevlm_heads *heads, void *stream);
+
+/*
+ * Attention of the newest tokens of every request over what the cache holds for it (their own K and V included, so they are stored
+ * before).  Request s holds seq_len[s] tokens; the last row_len[s] of them are rows row_start[s] .. of q, out and lse (q, out:
+ * [num_rows][Hq][D], contiguous; lse: fp32 [num_rows][Hq] or NULL).  A row at position p sees token j iff
+ *     j <= p  and  ( window[s] < 0  or  p - j < window[s]  or  j < sink_len[s] )
+ * (window NULL: all of them; sink_len NULL: 0): a sliding window and first tokens that stay visible.  Tokens on a page outside
+ * the pool are not seen.  A row that sees nothing gets zeros, and -inf in lse.  Rows of no request are left as they were, and so are those of a
+ * request whose rows do not lie within [0, num_rows).  seq_len is taken within [0, max_pages * page_size].  Table entries of
+ * pages without a visible token are not read.  Several requests may name the same pages, no two the same rows.
+ *
+ * The keys of a request are split over workgroups, and the parts merged, by the lengths of all requests: results are the same
+ * for the same arguments, not for a request in another batch.  Workspace: pevlm_cache_attn_workspace_bytes.
+ */
+size_t pevlm_cache_attn_workspace_bytes(const pevlm_heads *heads, int32_t num_seqs, int32_t num_rows);
+pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pevlm_cache *cache, const pevlm_heads *heads, int32_t num_rows,
+                                  const int32_t *row_start, const int32_t *row_len, const int32_t *seq_len, const int32_t *sink_len,
+                                  const int32_t *window, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Query rows per work item the kernels selected by `heads` use for the block-prefill call and for
  * the question call (-1 for an invalid descriptor). */
 int32_t pevlm_prefill_tile_rows(const pevlm_heads *heads);

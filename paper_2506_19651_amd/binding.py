@@ -36,6 +36,11 @@ class _CHeads(ctypes.Structure):
                 ("softmax_scale", ctypes.c_float)]
 
 
+class _CCache(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_seqs", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("block_table", ctypes.c_void_p)]
+
+
 class WorkItem(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("q_start", "q_rows", "full_start", "full_len", "diag_start",
                                               "diag_len", "seq", "reserved")]
@@ -139,6 +144,20 @@ def load_library():
         lib.pevlm_probe_tile_loop_bf16.argtypes = [vp, vp, ctypes.c_size_t, i32, i32, i32, ctypes.POINTER(ctypes.c_double), vp]
         lib.pevlm_probe_copy.restype = ctypes.c_int
         lib.pevlm_probe_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
+        CP, i64, size_t = ctypes.POINTER(_CCache), ctypes.c_int64, ctypes.c_size_t
+        lib.pevlm_cache_pool_bytes.restype = size_t
+        lib.pevlm_cache_pool_bytes.argtypes = [HP, i32, i32]
+        lib.pevlm_cache_slots_workspace_bytes.restype = size_t
+        lib.pevlm_cache_slots_workspace_bytes.argtypes = [i32]
+        lib.pevlm_cache_slots.restype = ctypes.c_int
+        lib.pevlm_cache_slots.argtypes = [CP, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, size_t, vp]
+        for fn in (lib.pevlm_cache_store_kv4, lib.pevlm_cache_load_kv4):
+            fn.restype = ctypes.c_int
+            fn.argtypes = [vp, vp, i64, i64, vp, i32, CP, HP, vp]
+        lib.pevlm_cache_attn_workspace_bytes.restype = size_t
+        lib.pevlm_cache_attn_workspace_bytes.argtypes = [HP, i32, i32]
+        lib.pevlm_cache_attn_kv4.restype = ctypes.c_int
+        lib.pevlm_cache_attn_kv4.argtypes = [vp, vp, vp, CP, HP, i32, vp, vp, vp, vp, vp, vp, size_t, vp]
         lib.pevlm_visible_pairs.restype = ctypes.c_int
         lib.pevlm_visible_pairs.argtypes = [LP] + [ctypes.POINTER(ctypes.c_int64)] * 3
         _lib = lib
@@ -502,3 +521,168 @@ def pevlm_visible_pairs(layout: Layout):
     a, b, c = ctypes.c_int64(), ctypes.c_int64(), ctypes.c_int64()
     _check(load_library().pevlm_visible_pairs(layout.ref(), ctypes.byref(a), ctypes.byref(b), ctypes.byref(c)))
     return a.value, b.value, c.value
+
+
+# ------------------------------------------------------------------------------------------ paged KV cache in 4 bits
+_TORCH = None  # (torch, {dtype code: torch dtype}, current_device, raw stream of a device)
+
+
+def _torch():
+    global _TORCH
+    if _TORCH is None:
+        import torch
+
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None:
+            raw = lambda device: torch.cuda.current_stream(device).cuda_stream  # noqa: E731
+        _TORCH = (torch, {PEVLM_F32: torch.float32, PEVLM_BF16: torch.bfloat16}, torch.cuda.current_device, raw)
+    return _TORCH
+
+
+def _refuse(message: str):
+    raise PevlmError(PEVLM_ERR_INVALID_ARG, message)
+
+
+class KvCache:
+    """Host-side descriptor of a paged 4-bit KV cache: the pool (device uint8 [num_pages][Hkv][page_size / 16][17 * head_dim], as
+    new_pool makes it) and the requests' block table (device int32 [num_seqs][max_pages]).  Holds on to both tensors."""
+
+    def __init__(self, pool, block_table, page_size: int):
+        torch = _torch()[0]
+        if pool.dtype != torch.uint8 or pool.dim() != 4 or not pool.is_contiguous() or pool.shape[2] * 16 != page_size or pool.shape[3] % 17:
+            _refuse(f"the pool must be a contiguous uint8 tensor [num_pages][Hkv][page_size / 16][17 * head_dim], got {tuple(pool.shape)} of "
+                    f"{pool.dtype} for pages of {page_size}")
+        if block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
+            _refuse("block_table must be a contiguous int32 tensor [num_seqs][max_pages]")
+        if pool.device != block_table.device:
+            _refuse("the pool and block_table are on different devices")
+        self.pool, self.block_table, self.page_size = pool, block_table, int(page_size)
+        self.num_pages, self.n_kv_heads, self.head_dim = int(pool.shape[0]), int(pool.shape[1]), int(pool.shape[3]) // 17
+        self.num_seqs, self.max_pages = int(block_table.shape[0]), int(block_table.shape[1])
+        self.device = pool.get_device()
+        self.struct = _CCache(pool.data_ptr(), self.num_pages, self.page_size, self.num_seqs, self.max_pages, block_table.data_ptr())
+        self._ref = ctypes.byref(self.struct)
+
+    @staticmethod
+    def new_pool(heads: "Heads", num_pages: int, page_size: int, device):
+        torch = _torch()[0]
+        if pevlm_cache_pool_bytes(heads, num_pages, page_size) == 0:
+            _refuse(pevlm_last_error())
+        return torch.zeros((num_pages, heads.n_kv_heads, page_size // 16, 17 * heads.head_dim), dtype=torch.uint8, device=device)
+
+    def ref(self):
+        return self._ref
+
+
+class _Call:
+    """What a call on a cache checks of its tensors, and the device and stream that it runs on."""
+
+    def __init__(self, cache: KvCache):
+        self.device = cache.device
+        self.torch, self.dtypes, self.current, self.raw = _torch()
+
+    def ints(self, name, t, count, optional=False):
+        """Address of a contiguous int32 array of `count` entries."""
+        if t is None:
+            if not optional:
+                _refuse(f"{name} must be given")
+            return None
+        if t.dtype is not self.torch.int32 or t.numel() != count or not t.is_contiguous():
+            _refuse(f"{name} must be a contiguous int32 tensor of {count} entries, got {tuple(t.shape)} of {t.dtype}")
+        return self.here(name, t)
+
+    def here(self, name, t):
+        if t.get_device() != self.device:
+            _refuse(f"{name} is on {t.device}, the cache on device {self.device}")
+        return t.data_ptr()
+
+    def run(self, fn, args, stream):
+        """fn(*args, stream) on the cache's device."""
+        if self.device < 0:
+            _refuse("the cache is not in device memory")
+        if self.device == self.current():
+            _check(fn(*args, self.raw(self.device) if stream is None else _stream_ptr(stream)))
+            return
+        with self.torch.cuda.device(self.device):
+            _check(fn(*args, self.raw(self.device) if stream is None else _stream_ptr(stream)))
+
+
+def _check_heads_of(cache: KvCache, heads: Heads):
+    if heads.n_kv_heads != cache.n_kv_heads or heads.head_dim != cache.head_dim:
+        _refuse(f"the cache holds {cache.n_kv_heads} KV heads of {cache.head_dim}, heads has {heads.n_kv_heads} of {heads.head_dim}")
+
+
+def pevlm_cache_pool_bytes(heads: Heads, num_pages: int, page_size: int) -> int:
+    return int(load_library().pevlm_cache_pool_bytes(heads.ref(), int(num_pages), int(page_size)))
+
+
+def pevlm_cache_slots_workspace_bytes(num_seqs: int) -> int:
+    return int(load_library().pevlm_cache_slots_workspace_bytes(int(num_seqs)))
+
+
+def pevlm_cache_slots(cache: KvCache, seq_len, new_len, free_pages, num_free, seq_len_out, num_free_out, row_start, row_len, slot_map,
+                      pos_ids=None, pos_offset=None, workspace=None, stream=None):
+    """Pages, slots and positions of the new tokens.  num_rows is slot_map's length; pos_ids: int32 [3][num_rows]."""
+    c, n, rows, free = _Call(cache), cache.num_seqs, slot_map.numel(), free_pages.numel()
+    args = [cache.ref(), c.ints("seq_len", seq_len, n), c.ints("new_len", new_len, n, True), c.ints("free_pages", free_pages, free), free,
+            c.ints("num_free", num_free, 1), rows, c.ints("pos_offset", pos_offset, n, True), c.ints("seq_len_out", seq_len_out, n),
+            c.ints("num_free_out", num_free_out, 1), c.ints("row_start", row_start, n), c.ints("row_len", row_len, n),
+            c.ints("slot_map", slot_map, rows), c.ints("pos_ids", pos_ids, 3 * rows, True)]
+    if workspace is None:
+        workspace = _workspace(pevlm_cache_slots_workspace_bytes(n), slot_map)
+    c.run(load_library().pevlm_cache_slots, args + [c.here("workspace", workspace), workspace.numel()], stream)
+    return workspace
+
+
+def _kv_rows(c: _Call, cache: KvCache, heads: Heads, rows: int, tensors):
+    """Addresses of k and v [rows][Hkv][D], whose rows may lie further apart, and their strides in elements."""
+    _check_heads_of(cache, heads)
+    dtype, inner = c.dtypes[heads.struct.dtype], cache.head_dim
+    shape, addresses, strides = (rows, cache.n_kv_heads, inner), [], []
+    for name, t in tensors:
+        if t.dtype is not dtype or t.shape != shape:
+            _refuse(f"{name} must be {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+        stride = t.stride()
+        if (stride[2] != 1 or (stride[1] != inner and shape[1] > 1)) and rows:
+            _refuse(f"a row of {name} must be contiguous (strides {stride})")
+        addresses.append(c.here(name, t))
+        strides.append(stride[0] if rows > 1 else 0)
+    return addresses + strides
+
+
+def pevlm_cache_store_kv4(k, v, slot_map, cache: KvCache, heads: Heads, stream=None):
+    """k, v: [rows][Hkv][D] of the dtype of heads, rows contiguous in themselves; slot_map: int32 [rows]."""
+    c, rows = _Call(cache), slot_map.numel()
+    args = _kv_rows(c, cache, heads, rows, (("k", k), ("v", v)))
+    c.run(load_library().pevlm_cache_store_kv4, args + [c.ints("slot_map", slot_map, rows), rows, cache.ref(), heads.ref()], stream)
+
+
+def pevlm_cache_load_kv4(k, v, slot_map, cache: KvCache, heads: Heads, stream=None):
+    """As pevlm_cache_store_kv4, the other way."""
+    c, rows = _Call(cache), slot_map.numel()
+    args = _kv_rows(c, cache, heads, rows, (("k", k), ("v", v)))
+    c.run(load_library().pevlm_cache_load_kv4, args + [c.ints("slot_map", slot_map, rows), rows, cache.ref(), heads.ref()], stream)
+
+
+def pevlm_cache_attn_workspace_bytes(heads: Heads, num_seqs: int, num_rows: int) -> int:
+    return int(load_library().pevlm_cache_attn_workspace_bytes(heads.ref(), int(num_seqs), int(num_rows)))
+
+
+def pevlm_cache_attn_kv4(q, out, cache: KvCache, heads: Heads, row_start, row_len, seq_len, sink_len=None, window=None, lse=None,
+                         workspace=None, stream=None):
+    """q, out: contiguous [rows][Hq][D] of the dtype of heads; lse: float32 [rows][Hq] or None."""
+    c, n = _Call(cache), cache.num_seqs
+    _check_heads_of(cache, heads)
+    shape, dtype = (q.shape[0], heads.n_q_heads, heads.head_dim), c.dtypes[heads.struct.dtype]
+    for name, t in (("q", q), ("out", out)):
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+            _refuse(f"{name} must be contiguous, [rows][{shape[1]}][{shape[2]}] of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+    if lse is not None and (lse.dtype is not c.torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous()):
+        _refuse(f"lse must be contiguous, {shape[:2]} of float32, got {tuple(lse.shape)} of {lse.dtype}")
+    if workspace is None:
+        workspace = _workspace(pevlm_cache_attn_workspace_bytes(heads, n, shape[0]), q)
+    args = [c.here("q", q), c.here("out", out), None if lse is None else c.here("lse", lse), cache.ref(), heads.ref(), shape[0],
+            c.ints("row_start", row_start, n), c.ints("row_len", row_len, n), c.ints("seq_len", seq_len, n),
+            c.ints("sink_len", sink_len, n, True), c.ints("window", window, n, True), c.here("workspace", workspace), workspace.numel()]
+    c.run(load_library().pevlm_cache_attn_kv4, args, stream)
+    return workspace

@@ -12,13 +12,14 @@
 #include <numeric>
 
 #include "common.h"
+#include "host.h"
 #include "rope_math.h"
 
 namespace pevlm {
 
 static thread_local char g_err[512] = "no error";
 
-static pevlm_status fail(pevlm_status st, const char *fmt, ...)
+pevlm_status fail(pevlm_status st, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -27,13 +28,10 @@ static pevlm_status fail(pevlm_status st, const char *fmt, ...)
     return st;
 }
 
-static pevlm_status hip_fail(hipError_t e, const char *what)
+pevlm_status hip_fail(hipError_t e, const char *what)
 {
     return fail(PEVLM_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
-
-static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-static size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
 static pevlm_status check_layout(const pevlm_layout *lay)
 {
@@ -55,7 +53,7 @@ static pevlm_status check_layout(const pevlm_layout *lay)
     return PEVLM_OK;
 }
 
-static pevlm_status check_heads(const pevlm_heads *h, HeadTable *tab)
+pevlm_status check_heads(const pevlm_heads *h, HeadTable *tab)
 {
     if (!h) return fail(PEVLM_ERR_INVALID_ARG, "heads is NULL");
     if (h->n_q_heads < 1 || h->n_kv_heads < 1 || h->n_q_heads % h->n_kv_heads != 0)
@@ -80,7 +78,7 @@ static pevlm_status check_heads(const pevlm_heads *h, HeadTable *tab)
     return PEVLM_OK;
 }
 
-static float scale_of(const pevlm_heads *h)
+float scale_of(const pevlm_heads *h)
 {
     return h->softmax_scale > 0.f ? h->softmax_scale : (float)(1.0 / sqrt((double)h->head_dim));
 }
@@ -409,8 +407,6 @@ static bool cut_by_cost(const SeqTable &tab, int32_t G, int32_t Hkv, StreamShare
     return worth_dealing(list, n, total, G, *sh);
 }
 
-static int32_t compute_units();
-
 // Stream items of the call if the streaming kernel is to run it, else 0.
 static int64_t stream_items_if_chosen(const pevlm_layout *lay, const pevlm_heads *h, const Restrict &r, bool fuse_rope)
 {
@@ -421,7 +417,7 @@ static int64_t stream_items_if_chosen(const pevlm_layout *lay, const pevlm_heads
 }
 
 // Compute units of the current device (256 when it cannot be queried, e.g. no GPU present).
-static int32_t compute_units()
+int32_t compute_units()
 {
     static std::atomic<int32_t> cached[16];  // zero-initialised; racing first calls store the same value
     int dev = 0;

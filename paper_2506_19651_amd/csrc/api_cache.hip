@@ -1,0 +1,193 @@
+// Host side of the paged KV cache: argument validation and launches.  Entry points are documented in include/pevlm.h.
+#include <string.h>
+
+#include <algorithm>
+
+#include "host.h"
+#include "kv4.h"
+
+namespace pevlm {
+
+constexpr int32_t kMinPage = 16, kMaxPage = 4096;
+
+static bool page_size_ok(int32_t n) { return n >= kMinPage && n <= kMaxPage && (n & (n - 1)) == 0; }
+
+static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+static pevlm_status check_pool(const pevlm_cache *c, Kv4Pool *pool, int32_t n_kv_heads)
+{
+    if (!c) return fail(PEVLM_ERR_INVALID_ARG, "cache is NULL");
+    if (!page_size_ok(c->page_size)) return fail(PEVLM_ERR_INVALID_ARG, "page_size %d is not a power of two in [%d, %d]", c->page_size, kMinPage, kMaxPage);
+    if (c->num_pages < 1 || (int64_t)c->num_pages * c->page_size > INT32_MAX)
+        return fail(PEVLM_ERR_INVALID_ARG, "num_pages %d of %d tokens: need >= 1 page and fewer than 2^31 tokens", c->num_pages, c->page_size);
+    pool->base = (uint8_t *)c->pool;
+    pool->num_pages = c->num_pages;
+    pool->page_shift = __builtin_ctz(c->page_size);
+    pool->n_kv_heads = n_kv_heads;
+    return PEVLM_OK;
+}
+
+static pevlm_status check_pool_memory(const pevlm_cache *c)
+{
+    if (!c->pool || !aligned16(c->pool)) return fail(PEVLM_ERR_INVALID_ARG, "the pool must be a 16-byte aligned device pointer");
+    return PEVLM_OK;
+}
+
+static pevlm_status check_table(const pevlm_cache *c)
+{
+    if (c->num_seqs < 1 || c->max_pages < 1 || (int64_t)c->max_pages * c->page_size > INT32_MAX)
+        return fail(PEVLM_ERR_INVALID_ARG, "block table [%d][%d] of pages of %d tokens: need >= 1 request, >= 1 column and fewer than 2^31 tokens a request",
+                    c->num_seqs, c->max_pages, c->page_size);
+    if (!c->block_table || !aligned4(c->block_table)) return fail(PEVLM_ERR_INVALID_ARG, "block_table must be a 4-byte aligned device pointer");
+    return PEVLM_OK;
+}
+
+static pevlm_status check_rows(const void *k, const void *v, int64_t k_stride, int64_t v_stride, const int32_t *slot_map, int32_t num_rows,
+                               const pevlm_cache *cache, const pevlm_heads *heads, Kv4Rows *p)
+{
+    pevlm_status st = check_heads(heads, nullptr);
+    if (st != PEVLM_OK) return st;
+    st = check_pool(cache, &p->pool, heads->n_kv_heads);
+    if (st != PEVLM_OK) return st;
+    if (num_rows < 0) return fail(PEVLM_ERR_INVALID_ARG, "num_rows must not be negative");
+    const int64_t row = (int64_t)heads->n_kv_heads * heads->head_dim;
+    for (int64_t stride : {k_stride, v_stride})
+        if (stride != 0 && (stride < row || stride % 8 != 0 || stride > INT32_MAX))
+            return fail(PEVLM_ERR_INVALID_ARG, "row stride %lld: need 0 or a multiple of 8 of at least %lld, below 2^31", (long long)stride, (long long)row);
+    if (num_rows == 0) return PEVLM_OK;
+    st = check_pool_memory(cache);
+    if (st != PEVLM_OK) return st;
+    if (!k || !v || !aligned16(k) || !aligned16(v)) return fail(PEVLM_ERR_INVALID_ARG, "k and v must be 16-byte aligned device pointers");
+    if (!slot_map || !aligned4(slot_map)) return fail(PEVLM_ERR_INVALID_ARG, "slot_map must be a 4-byte aligned device pointer");
+    p->k = (void *)k;
+    p->v = (void *)v;
+    p->k_stride = k_stride ? k_stride : row;
+    p->v_stride = v_stride ? v_stride : row;
+    p->slot_map = slot_map;
+    p->num_rows = num_rows;
+    return PEVLM_OK;
+}
+
+}  // namespace pevlm
+
+using namespace pevlm;
+
+extern "C" {
+
+size_t pevlm_cache_pool_bytes(const pevlm_heads *heads, int32_t num_pages, int32_t page_size)
+{
+    Kv4Pool pool;
+    pevlm_cache c = {};
+    c.num_pages = num_pages;
+    c.page_size = page_size;
+    if (check_heads(heads, nullptr) != PEVLM_OK || check_pool(&c, &pool, heads->n_kv_heads) != PEVLM_OK) return 0;
+    return (size_t)num_pages * heads->n_kv_heads * (page_size / kKv4Record) * 17 * heads->head_dim;
+}
+
+size_t pevlm_cache_slots_workspace_bytes(int32_t num_seqs)
+{
+    if (num_seqs < 1) {
+        fail(PEVLM_ERR_INVALID_ARG, "num_seqs must be >= 1");
+        return 0;
+    }
+    return align256((size_t)num_seqs * sizeof(int32_t)) + 256;
+}
+
+pevlm_status pevlm_cache_slots(const pevlm_cache *cache, const int32_t *seq_len, const int32_t *new_len, const int32_t *free_pages,
+                               int32_t free_capacity, const int32_t *num_free, int32_t num_rows, const int32_t *pos_offset, int32_t *seq_len_out,
+                               int32_t *num_free_out, int32_t *row_start, int32_t *row_len, int32_t *slot_map, int32_t *pos_ids,
+                               void *workspace, size_t workspace_bytes, void *stream)
+{
+    Kv4Pool pool;
+    pevlm_status st = check_pool(cache, &pool, 1);
+    if (st == PEVLM_OK) st = check_table(cache);
+    if (st != PEVLM_OK) return st;
+    if (num_rows < 0 || free_capacity < 0) return fail(PEVLM_ERR_INVALID_ARG, "num_rows and free_capacity must not be negative");
+    if (!seq_len || !num_free || !seq_len_out || !num_free_out || !row_start || !row_len || (!free_pages && free_capacity > 0) || (!slot_map && num_rows > 0))
+        return fail(PEVLM_ERR_INVALID_ARG, "only new_len, pos_offset and pos_ids (and arrays without an entry) may be NULL");
+    for (const int32_t *a : {seq_len, new_len, free_pages, num_free, pos_offset, (const int32_t *)seq_len_out, (const int32_t *)num_free_out,
+                             (const int32_t *)row_start, (const int32_t *)row_len, (const int32_t *)slot_map, (const int32_t *)pos_ids})
+        if (!aligned4(a)) return fail(PEVLM_ERR_INVALID_ARG, "arrays must be 4-byte aligned");
+    const size_t need = (size_t)cache->num_seqs * sizeof(int32_t);
+    if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))
+        return fail(PEVLM_ERR_WORKSPACE_TOO_SMALL, "slots workspace needs %zu bytes, 256-byte aligned (got %zu)",
+                    pevlm_cache_slots_workspace_bytes(cache->num_seqs), workspace ? workspace_bytes : (size_t)0);
+    Kv4Slots p;
+    p.seq_len = seq_len; p.new_len = new_len; p.free_pages = free_pages; p.num_free = num_free; p.pos_offset = pos_offset;
+    p.seq_len_out = seq_len_out; p.num_free_out = num_free_out; p.row_start = row_start; p.row_len = row_len;
+    p.slot_map = slot_map; p.pos_ids = pos_ids; p.table = cache->block_table;
+    p.first_free = (int32_t *)workspace;
+    p.num_seqs = cache->num_seqs;
+    p.num_rows = num_rows;
+    p.max_pages = cache->max_pages;
+    p.page_shift = pool.page_shift;
+    p.num_pages = cache->num_pages;
+    p.free_capacity = free_capacity;
+    const hipError_t e = launch_kv4_slots(p, (hipStream_t)stream);
+    return e == hipSuccess ? PEVLM_OK : hip_fail(e, "slots launch");
+}
+
+pevlm_status pevlm_cache_store_kv4(const void *k, const void *v, int64_t k_stride, int64_t v_stride, const int32_t *slot_map, int32_t num_rows,
+                                   const pevlm_cache *cache, const pevlm_heads *heads, void *stream)
+{
+    Kv4Rows p;
+    const pevlm_status st = check_rows(k, v, k_stride, v_stride, slot_map, num_rows, cache, heads, &p);
+    if (st != PEVLM_OK || num_rows == 0) return st;
+    const hipError_t e = launch_kv4_store(p, heads->head_dim, heads->dtype == PEVLM_BF16, (hipStream_t)stream);
+    return e == hipSuccess ? PEVLM_OK : hip_fail(e, "cache store launch");
+}
+
+pevlm_status pevlm_cache_load_kv4(void *k, void *v, int64_t k_stride, int64_t v_stride, const int32_t *slot_map, int32_t num_rows,
+                                  const pevlm_cache *cache, const pevlm_heads *heads, void *stream)
+{
+    Kv4Rows p;
+    const pevlm_status st = check_rows(k, v, k_stride, v_stride, slot_map, num_rows, cache, heads, &p);
+    if (st != PEVLM_OK || num_rows == 0) return st;
+    const hipError_t e = launch_kv4_load(p, heads->head_dim, heads->dtype == PEVLM_BF16, (hipStream_t)stream);
+    return e == hipSuccess ? PEVLM_OK : hip_fail(e, "cache load launch");
+}
+
+size_t pevlm_cache_attn_workspace_bytes(const pevlm_heads *heads, int32_t num_seqs, int32_t num_rows)
+{
+    if (check_heads(heads, nullptr) != PEVLM_OK) return 0;
+    if (num_seqs < 1 || num_rows < 0) {
+        fail(PEVLM_ERR_INVALID_ARG, "need num_seqs >= 1 and num_rows >= 0");
+        return 0;
+    }
+    return 256;
+}
+
+pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pevlm_cache *cache, const pevlm_heads *heads, int32_t num_rows,
+                                  const int32_t *row_start, const int32_t *row_len, const int32_t *seq_len, const int32_t *sink_len,
+                                  const int32_t *window, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Kv4Attn p;
+    memset(&p, 0, sizeof p);
+    pevlm_status st = check_heads(heads, &p.heads);
+    if (st == PEVLM_OK) st = check_pool(cache, &p.pool, heads->n_kv_heads);
+    if (st == PEVLM_OK) st = check_table(cache);
+    if (st == PEVLM_OK) st = check_pool_memory(cache);
+    if (st != PEVLM_OK) return st;
+    if (num_rows < 0) return fail(PEVLM_ERR_INVALID_ARG, "num_rows must not be negative");
+    if (num_rows == 0) return PEVLM_OK;
+    if (!q || !out || !aligned16(q) || !aligned16(out)) return fail(PEVLM_ERR_INVALID_ARG, "q and out must be 16-byte aligned device pointers");
+    if (!row_start || !row_len || !seq_len) return fail(PEVLM_ERR_INVALID_ARG, "row_start, row_len and seq_len must not be NULL");
+    for (const int32_t *a : {row_start, row_len, seq_len, sink_len, window, (const int32_t *)lse})
+        if (!aligned4(a)) return fail(PEVLM_ERR_INVALID_ARG, "arrays must be 4-byte aligned");
+    const size_t need = 0;
+    if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))
+        return fail(PEVLM_ERR_WORKSPACE_TOO_SMALL, "cache attention workspace needs %zu bytes, 256-byte aligned (got %zu)",
+                    pevlm_cache_attn_workspace_bytes(heads, cache->num_seqs, num_rows), workspace ? workspace_bytes : (size_t)0);
+    p.q = q; p.out = out; p.lse = lse;
+    p.table = cache->block_table;
+    p.row_start = row_start; p.row_len = row_len; p.seq_len = seq_len; p.sink_len = sink_len; p.window = window;
+    p.num_seqs = cache->num_seqs;
+    p.max_pages = cache->max_pages;
+    p.num_rows = num_rows;
+    p.n_q_heads = heads->n_q_heads;
+    p.scale = scale_of(heads);
+    const hipError_t e = launch_attn_kv4(p, heads->head_dim, heads->dtype == PEVLM_BF16, (hipStream_t)stream);
+    return e == hipSuccess ? PEVLM_OK : hip_fail(e, "cache attention launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,79 @@
+// The paged 4-bit KV cache: its format as the kernels see it, and what the entry points hand to them.
+#pragma once
+#include "common.h"
+
+namespace pevlm {
+
+constexpr int32_t kKv4Record = 16;                 // tokens of a record
+constexpr int32_t kKv4MinExp = -100, kKv4MaxExp = 125;
+constexpr int32_t kKv4Bias = 127, kKv4NanScale = 255;
+
+template <int D>
+struct Kv4Cfg {
+    static constexpr int NB = D / 32;              // blocks of a token's row
+    static constexpr int CODES = 8 * D;            // bytes of a record's K (or V) codes
+    static constexpr int SCALES = 16 * D;          // where its scales begin
+    static constexpr int BYTES = 17 * D;
+};
+
+struct Kv4Pool {
+    uint8_t *base;
+    int32_t num_pages, page_shift, n_kv_heads;
+};
+
+// Record of the given page, KV head and record of the page.  A pool passes 2^32 bytes.
+template <int D>
+__host__ __device__ inline int64_t kv4_record(const Kv4Pool &p, int32_t page, int32_t head, int32_t r)
+{
+    return ((((int64_t)page * p.n_kv_heads + head) << (p.page_shift - 4)) + r) * Kv4Cfg<D>::BYTES;
+}
+
+// 2^e as a float, -126 <= e <= 127
+__device__ __forceinline__ float exp2_int(int32_t e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Scale of a block from its byte; bytes that no store writes give what they say, 0 the nearest normal number
+__device__ __forceinline__ float kv4_scale(uint32_t byte)
+{
+    return __uint_as_float(byte == kKv4NanScale ? 0x7fc00000u : (byte ? byte : 1u) << 23);
+}
+
+__device__ __forceinline__ float kv4_value(uint32_t code)  // of the low four bits
+{
+    const uint32_t m = code & 7u;
+    // 0, 1/2: m / 2; from 1 on one mantissa bit under an exponent
+    const float x = m < 2 ? 0.5f * m : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
+    return code & 8u ? -x : x;
+}
+
+struct Kv4Slots {
+    const int32_t *seq_len, *new_len, *free_pages, *num_free, *pos_offset;
+    int32_t *seq_len_out, *num_free_out, *row_start, *row_len, *slot_map, *pos_ids, *table;
+    int32_t *first_free;  // [num_seqs] scratch: where in the list the request's first new page stands (the others before it)
+    int32_t num_seqs, num_rows, max_pages, page_shift, num_pages, free_capacity;
+};
+
+struct Kv4Rows {  // rows of K and V that go into slots, or come out of them
+    void *k, *v;
+    int64_t k_stride, v_stride;  // elements
+    const int32_t *slot_map;
+    int32_t num_rows;
+    Kv4Pool pool;
+};
+
+struct Kv4Attn {
+    const void *q;
+    void *out;
+    float *lse;
+    Kv4Pool pool;
+    const int32_t *table, *row_start, *row_len, *seq_len, *sink_len, *window;
+    int32_t num_seqs, max_pages, num_rows, n_q_heads;
+    float scale;
+    HeadTable heads;
+};
+
+hipError_t launch_kv4_slots(const Kv4Slots &p, hipStream_t stream);
+hipError_t launch_kv4_store(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream);
+hipError_t launch_kv4_load(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream);
+hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, hipStream_t stream);
+
+}  // namespace pevlm
