@@ -68,6 +68,37 @@ static pevlm_status check_rows(const void *k, const void *v, int64_t k_stride, i
     return PEVLM_OK;
 }
 
+// Query heads by KV head; returns the largest group
+static int32_t group_heads(const HeadTable &tab, const pevlm_heads *h, Kv4Heads *out)
+{
+    int32_t most = 0, n = 0;
+    for (int32_t g = 0; g < h->n_kv_heads; ++g) {
+        out->first[g] = (uint16_t)n;
+        while (n < h->n_q_heads && tab.kv_of_q[tab.head_order[n]] == g) ++n;
+        most = std::max(most, n - out->first[g]);
+    }
+    out->first[h->n_kv_heads] = (uint16_t)n;
+    memcpy(out->order, tab.head_order, sizeof out->order);
+    return most;
+}
+
+// What bounds a call's items, and how it is cut.  A request with r rows has ceil(r * group / kKv4Pairs) tiles of a KV head.
+static void size_attn(const pevlm_heads *h, int32_t num_seqs, int32_t num_rows, Kv4Attn *p)
+{
+    HeadTable tab;
+    check_heads(h, &tab);
+    p->group = group_heads(tab, h, &p->heads);
+    const int64_t asking = std::min(num_seqs, num_rows);
+    const int64_t units = h->n_kv_heads * (asking + (int64_t)num_rows * p->group / kKv4Pairs);
+    p->target_items = 2 * compute_units();
+    p->min_steps = 16;
+    p->max_units = (int32_t)std::min<int64_t>(units, INT32_MAX);
+    p->max_items = (int32_t)std::min<int64_t>(units + p->target_items, INT32_MAX);
+}
+
+static size_t ml_bytes(const Kv4Attn &p) { return align256((size_t)p.max_items * kKv4Pairs * 2 * sizeof(float)); }
+static size_t attn_bytes(const Kv4Attn &p, int32_t D) { return ml_bytes(p) + align256((size_t)p.max_items * kKv4Pairs * D * sizeof(float)); }
+
 }  // namespace pevlm
 
 using namespace pevlm;
@@ -154,7 +185,9 @@ size_t pevlm_cache_attn_workspace_bytes(const pevlm_heads *heads, int32_t num_se
         fail(PEVLM_ERR_INVALID_ARG, "need num_seqs >= 1 and num_rows >= 0");
         return 0;
     }
-    return 256;
+    Kv4Attn p;
+    size_attn(heads, num_seqs, num_rows, &p);
+    return attn_bytes(p, heads->head_dim) + 256;
 }
 
 pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pevlm_cache *cache, const pevlm_heads *heads, int32_t num_rows,
@@ -163,7 +196,7 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
 {
     Kv4Attn p;
     memset(&p, 0, sizeof p);
-    pevlm_status st = check_heads(heads, &p.heads);
+    pevlm_status st = check_heads(heads, nullptr);
     if (st == PEVLM_OK) st = check_pool(cache, &p.pool, heads->n_kv_heads);
     if (st == PEVLM_OK) st = check_table(cache);
     if (st == PEVLM_OK) st = check_pool_memory(cache);
@@ -174,7 +207,9 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
     if (!row_start || !row_len || !seq_len) return fail(PEVLM_ERR_INVALID_ARG, "row_start, row_len and seq_len must not be NULL");
     for (const int32_t *a : {row_start, row_len, seq_len, sink_len, window, (const int32_t *)lse})
         if (!aligned4(a)) return fail(PEVLM_ERR_INVALID_ARG, "arrays must be 4-byte aligned");
-    const size_t need = 0;
+    size_attn(heads, cache->num_seqs, num_rows, &p);
+    if (p.max_items > 0x3fffffff || (int64_t)p.max_units * kKv4Pairs > INT32_MAX) return fail(PEVLM_ERR_UNSUPPORTED, "too many work items");
+    const size_t need = attn_bytes(p, heads->head_dim);
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))
         return fail(PEVLM_ERR_WORKSPACE_TOO_SMALL, "cache attention workspace needs %zu bytes, 256-byte aligned (got %zu)",
                     pevlm_cache_attn_workspace_bytes(heads, cache->num_seqs, num_rows), workspace ? workspace_bytes : (size_t)0);
@@ -185,8 +220,12 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
     p.max_pages = cache->max_pages;
     p.num_rows = num_rows;
     p.n_q_heads = heads->n_q_heads;
-    p.scale = scale_of(heads);
-    const hipError_t e = launch_attn_kv4(p, heads->head_dim, heads->dtype == PEVLM_BF16, (hipStream_t)stream);
+    p.part_ml = (float *)workspace;
+    p.part_acc = (float *)((char *)workspace + ml_bytes(p));
+    p.c_log2 = scale_of(heads) * 1.4426950408889634f;
+    // a table too short for a second item of a unit leaves nothing to merge
+    const bool merge = (int64_t)cache->max_pages * cache->page_size > (int64_t)p.min_steps * kKv4Step;
+    const hipError_t e = launch_attn_kv4(p, heads->head_dim, heads->dtype == PEVLM_BF16, merge, (hipStream_t)stream);
     return e == hipSuccess ? PEVLM_OK : hip_fail(e, "cache attention launch");
 }
 

@@ -1,117 +1,531 @@
 // Attention over the paged 4-bit KV cache (gfx950).
 //
-// One wavefront per (row, query head): 64 keys a step, one to a lane; scores, a running maximum and sum of the softmax, then every
-// lane adds up D / 64 elements of the values.  All products and sums are in fp32.
+// Products run on the bf16 matrix cores: a code times its block's scale is a bf16 number exactly (v_cvt_scalef32_pk_bf16_fp4, two
+// values an instruction).  Scores are formed transposed, S^T = K Q^T (v_mfma_f32_16x16x32_bf16): the wavefront-wide 16-byte load of
+// a record's K codes gives a lane one block of 32 elements of one key under one scale, which is its share of the A operand if
+// the k index runs over the blocks first; a lane then has four keys of one (row, head) pair in its accumulators, and the weights
+// of two records are its share of the B operand of O^T += V^T P^T.  V comes by the same load, goes as bf16 through a slice of LDS of
+// the wavefront's own and back transposed (ds_read_b64_tr_b16).
+//
+// Roundings: Q of fp32 tensors is split into three bf16 parts that add up to it, weights into two (bf16 tensors, 2^-16) or three
+// parts (fp32); products of parts are exact in fp32, sums are fp32 throughout.
+#include "bf16_device.h"
 #include "kv4.h"
 
 namespace pevlm {
 
-template <bool BF16>
-__device__ __forceinline__ float attn_element(const void *p, int64_t i)
+namespace {
+
+constexpr int NW = 8;  // wavefronts of a workgroup
+constexpr int32_t kMany = 0x3fffffff;
+
+// What a request's rows see: records (16 tokens) [0, n_sink) and [near, near + n_near), which do not overlap
+struct Span {
+    int32_t n_sink, near, records;
+};
+
+struct Request {
+    int32_t row0, rows, held, sink;  // rows: 0 if it has none (to write)
+    int32_t window;                  // < 0: none
+};
+
+__device__ __forceinline__ Request read_request(const Kv4Attn &p, int32_t s)
 {
-    return BF16 ? __uint_as_float((uint32_t)((const uint16_t *)p)[i] << 16) : ((const float *)p)[i];
+    Request r;
+    const int64_t width = (int64_t)p.max_pages << p.pool.page_shift;
+    r.row0 = p.row_start[s];
+    r.rows = p.row_len[s];
+    const int32_t len = p.seq_len[s];
+    r.held = len < 0 ? 0 : (len < width ? len : (int32_t)width);
+    r.window = p.window ? p.window[s] : -1;
+    r.sink = p.sink_len && r.window >= 0 ? p.sink_len[s] : 0;
+    r.sink = r.sink < 0 ? 0 : (r.sink < r.held ? r.sink : r.held);
+    if (r.row0 < 0 || r.rows < 0 || (int64_t)r.row0 + r.rows > p.num_rows) r.rows = 0;
+    return r;
 }
 
-__device__ __forceinline__ uint16_t bf16_nearest(float f)
+// first token inside the window of the token at position `pos`
+__device__ __forceinline__ int32_t near_of(const Request &r, int32_t pos)
 {
-    uint32_t u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0;
-    u += 0x7fffu + ((u >> 16) & 1u);
-    return (uint16_t)(u >> 16);
+    const int64_t n = (int64_t)pos - r.window + 1;
+    return r.window < 0 || n < 0 ? 0 : (int32_t)(n < r.held ? n : r.held);
 }
+
+__device__ __forceinline__ Span span_of(const Request &r)
+{
+    Span s;
+    const int32_t first = near_of(r, r.held - r.rows);  // of the earliest row; a row before the first token sees nothing
+    s.n_sink = ceil_div(r.sink, kKv4Record);
+    s.near = first / kKv4Record;
+    if (s.near < s.n_sink) s.near = s.n_sink;
+    const int32_t end = ceil_div(r.held, kKv4Record);
+    s.records = s.n_sink + (first < r.held && end > s.near ? end - s.near : 0);
+    return s;
+}
+
+__device__ __forceinline__ int32_t steps_of(const Span &s) { return ceil_div(s.records, kKv4Step / kKv4Record); }
+
+__device__ __forceinline__ int64_t wave_sum(int64_t x)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    return x;
+}
+
+__device__ __forceinline__ int32_t lane_value(int32_t x, int32_t lane) { return __builtin_amdgcn_readlane(x, lane); }
+
+// Where the idx-th item (or unit) of a call lies.  Every wavefront finds its own by itself: lane by lane over 64 requests at a
+// time, once for the whole work, which sets the items' length, and once for the place.
+struct Place {
+    int32_t s, first_item, splits, tiles, rest;  // rest: the item's (unit's) place within the request
+    Request r;
+};
+
+template <bool UNITS>
+__device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx_of_xcd, bool by_xcd)
+{
+    const int32_t lane = threadIdx.x & 63;
+    int64_t work = 0;
+    Request r;
+    int32_t steps = 0, tiles = 0;
+    const auto look = [&](int32_t s) {
+        steps = tiles = 0;
+        if (s < p.num_seqs) {
+            r = read_request(p, s);
+            if (r.rows > 0) {
+                tiles = (int32_t)(((int64_t)r.rows * p.group + kKv4Pairs - 1) / kKv4Pairs);
+                steps = steps_of(span_of(r));
+            }
+        }
+    };
+    for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
+        look(s0 + lane);
+        work += (int64_t)tiles * steps;
+    }
+    work = wave_sum(work) * p.pool.n_kv_heads;
+    int64_t length = (work + p.target_items - 1) / p.target_items;  // steps of an item
+    length = length > p.min_steps ? length : p.min_steps;
+    const int32_t per = (int32_t)(length < INT32_MAX ? length : INT32_MAX);
+
+    // Counts stop at kMany: with row ranges that overlap they can pass any bound, and no item or unit lies there
+    const auto count = [&](int32_t n) {
+        const int64_t x = (int64_t)n * tiles * p.pool.n_kv_heads;
+        return (int32_t)(x < kMany ? x : kMany);
+    };
+    const auto sum = [](int32_t a, int32_t b) { return a + b < kMany ? a + b : kMany; };
+    Place at;
+    at.s = -1;
+    at.first_item = 0;
+    int32_t before = 0;
+    int32_t idx = idx_of_xcd;
+    if (by_xcd) {  // all items, to deal contiguous eighths of them to the XCDs
+        int64_t items = 0;
+        for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
+            if (p.num_seqs > 64) look(s0 + lane);
+            items += count(steps ? ceil_div(steps, per) : 1);
+        }
+        items = wave_sum(items);
+        const int32_t all = (int32_t)(items < p.max_items ? items : p.max_items), per_xcd = (all + 7) / 8;
+        idx = (idx & 7) * per_xcd + (idx >> 3);
+        if (idx_of_xcd >> 3 >= per_xcd || idx >= all) return at;
+    }
+    for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
+        if (p.num_seqs > 64) look(s0 + lane);
+        const int32_t splits = steps ? ceil_div(steps, per) : 1;  // rows that see nothing are an item, too
+        const int32_t items = count(splits), mine = UNITS ? count(1) : items;
+        int32_t end = mine, item_end = items;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int32_t y = __shfl_up(end, o), z = __shfl_up(item_end, o);
+            if (lane >= o) {
+                end = sum(end, y);
+                item_end = sum(item_end, z);
+            }
+        }
+        const uint64_t found = __ballot(sum(before, end) > idx);
+        if (found) {
+            const int32_t f = __builtin_ctzll(found);
+            at.s = s0 + f;
+            at.rest = idx - before - (lane_value(end, f) - lane_value(mine, f));
+            at.splits = lane_value(splits, f);
+            at.tiles = lane_value(tiles, f);
+            at.first_item = sum(at.first_item, lane_value(item_end, f) - lane_value(items, f));
+            at.r.row0 = lane_value(r.row0, f);
+            at.r.rows = lane_value(r.rows, f);
+            at.r.held = lane_value(r.held, f);
+            at.r.sink = lane_value(r.sink, f);
+            at.r.window = lane_value(r.window, f);
+            return at;
+        }
+        before = sum(before, lane_value(end, 63));
+        at.first_item = sum(at.first_item, lane_value(item_end, 63));
+    }
+    return at;
+}
+
+__device__ __forceinline__ uint16_t bf16_nearest(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
+
+// N bf16 parts of two numbers; each takes the upper 8 bits of what the parts before it leave
+template <int N>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&part)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bf16x2 two = {(__bf16)a, (__bf16)b};
+        part[i] = __builtin_bit_cast(uint32_t, two);
+        if (i + 1 < N) {
+            a -= __uint_as_float(part[i] << 16);
+            b -= __uint_as_float(part[i] & 0xffff0000u);
+        }
+    }
+}
+
+constexpr float kStep = 8.f;  // base-2 units that a row's maximum may outgrow its reference by
+
+}  // namespace
 
 template <int D, bool BF16>
-__global__ __launch_bounds__(64) void attn_kv4_kernel(Kv4Attn p)
+__global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
 {
     using C = Kv4Cfg<D>;
-    __shared__ float query[D];
-    const int32_t row = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
-    int32_t s = -1, i = 0;
-    for (int32_t s0 = 0; s0 < p.num_seqs && s < 0; s0 += 64) {
-        const int32_t mine = s0 + lane;
-        bool has = false;
-        if (mine < p.num_seqs) {
-            const int64_t first = p.row_start[mine], n = p.row_len[mine];
-            has = first >= 0 && n > 0 && first + n <= p.num_rows && row >= first && row < first + n;
-        }
-        const uint64_t found = __ballot(has);
-        if (found) s = s0 + __builtin_ctzll(found);
-    }
-    if (s < 0) return;
-    i = row - p.row_start[s];
-    const int64_t width = (int64_t)p.max_pages << p.pool.page_shift;
-    const int32_t given = p.seq_len[s], held = given < 0 ? 0 : (given < width ? given : (int32_t)width);
-    const int32_t pos = held - p.row_len[s] + i;
-    const int32_t sink = p.sink_len ? p.sink_len[s] : 0, window = p.window ? p.window[s] : -1;
-    const int64_t near = window < 0 ? 0 : (int64_t)pos - window + 1;  // first token inside the window
-    const int32_t g = p.heads.kv_of_q[h];
-    for (int32_t d = lane; d < D; d += 64) query[d] = attn_element<BF16>(p.q, ((int64_t)row * p.n_q_heads + h) * D + d);
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, acc[D / 64];
-    for (int e = 0; e < D / 64; ++e) acc[e] = 0.f;
-    for (int32_t j0 = 0; j0 <= pos; j0 += 64) {
-        if (j0 >= sink && j0 + 63 < near) continue;
-        const int32_t j = j0 + lane, column = j >> p.pool.page_shift, in_page = j & ((1 << p.pool.page_shift) - 1);
-        bool seen = j <= pos && (j >= near || j < sink);
-        int32_t page = 0;
-        if (seen) {
-            page = p.table[(int64_t)s * p.max_pages + column];
-            seen = page >= 0 && page < p.pool.num_pages;
-        }
-        const int64_t rec = kv4_record<D>(p.pool, seen ? page : 0, g, in_page / kKv4Record);
-        const int32_t t = in_page % kKv4Record;
-        float score = -INFINITY;
-        if (seen) {
-            float sum = 0.f;
-            for (int b = 0; b < C::NB; ++b) {
-                const uint8_t *codes = p.pool.base + rec + (b * 16 + t) * 16;
-                const float scale = kv4_scale(p.pool.base[rec + C::SCALES + (b * 16 + t) * 2]);
-                for (int k = 0; k < 16; ++k) {
-                    sum += kv4_value(codes[k]) * scale * query[b * 32 + 2 * k];
-                    sum += kv4_value(codes[k] >> 4) * scale * query[b * 32 + 2 * k + 1];
+    constexpr int KS = D / 32;         // k-steps of a score
+    constexpr int DT = D / 16;         // tiles of 16 elements of an output row
+    constexpr int NQ = BF16 ? 1 : 3, NP = BF16 ? 2 : 3;
+    constexpr int ROWB = 2 * D;        // bytes of a V row in LDS
+    constexpr int CH = ROWB / 16;      // its 16-byte chunks
+    constexpr int WORDS = D / 32;      // words of codes of a lane: 32 (16) elements of D = 128 (64)
+    static_assert(WORDS == KS, "a lane's word is its share of a k-step");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[NW * 32 * ROWB];
+    __shared__ float lds_ml[NW][kKv4Pairs][2];
+
+    const Place at = find_place<false>(p, blockIdx.x, true);
+    if (at.s < 0) return;
+    const Request r = at.r;
+    const int32_t tile = at.rest % at.tiles, split = at.rest / at.tiles % at.splits, g = at.rest / (at.tiles * at.splits);
+    const int32_t item = at.first_item + at.rest;
+    const int32_t head0 = p.heads.first[g], G = p.heads.first[g + 1] - head0;
+    const int32_t pair0 = tile * kKv4Pairs, n_pairs_all = r.rows * G;
+    const int32_t n_pairs = n_pairs_all - pair0 < kKv4Pairs ? n_pairs_all - pair0 : kKv4Pairs;
+    if (n_pairs <= 0) return;
+    const Span span = span_of(r);
+    const int32_t steps = steps_of(span), per = ceil_div(steps, at.splits);
+    const int32_t step0 = split * per, step1 = step0 + per < steps ? step0 + per : steps;
+
+    const int32_t tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, kg = lane >> 4;
+    const int32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint8_t *const slice = lds + wave * 32 * ROWB;
+
+    // this lane's pair (column of S^T)
+    const int32_t pair = pair0 + (l16 < n_pairs ? l16 : n_pairs - 1);
+    const int32_t row = pair / G, head = p.heads.order[head0 + pair - row * G];
+    const int32_t pos = r.held - r.rows + row, near = near_of(r, pos);
+    // the tile's first and last rows: positions and windows rise with the row
+    const int32_t pos_lo = r.held - r.rows + pair0 / G, pos_hi = r.held - r.rows + (pair0 + n_pairs - 1) / G;
+    const int32_t near_lo = near_of(r, pos_lo), near_hi = near_of(r, pos_hi);
+
+    // ---- queries: the lane's pair, elements kg * (D / 4) + 8 m .. + 8 of k-step m
+    bf16x8 qf[NQ][KS];
+    {
+        const int64_t at_q = ((int64_t)(r.row0 + row) * p.n_q_heads + head) * D + kg * (D / 4);
+#pragma unroll
+        for (int m = 0; m < KS; ++m) {
+            if constexpr (BF16) {
+                qf[0][m] = *reinterpret_cast<const bf16x8 *>((const uint16_t *)p.q + at_q + m * 8);
+            } else {
+                const float *q = (const float *)p.q + at_q + m * 8;
+                uint32_t w[NQ][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t part[NQ];
+                    split_pair<NQ>(q[2 * i], q[2 * i + 1], part);
+                    for (int n = 0; n < NQ; ++n) w[n][i] = part[n];
+                }
+                for (int n = 0; n < NQ; ++n) {
+                    const uint4 v = make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
+                    qf[n][m] = __builtin_bit_cast(bf16x8, v);
                 }
             }
-            score = sum * p.scale;
         }
-        float top = score;
-        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.f : m_new;
-        const float w = seen ? expf(score - base) : 0.f, alpha = expf(m - base);
-        l *= alpha;
-        for (int e = 0; e < D / 64; ++e) acc[e] *= alpha;
-        m = m_new;
-        float sum = w;
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-        l += sum;
-        const uint64_t keys = __ballot(seen);
-        for (int k = 0; k < 64; ++k) {
-            if (!(keys >> k & 1)) continue;
-            const float wk = __shfl(w, k);
-            const int64_t r = __shfl(rec, k);
-            const int32_t tk = __shfl(t, k);
-            for (int e = 0; e < D / 64; ++e) {
-                const int32_t d = lane * (D / 64) + e, b = d / 32;
-                const uint32_t byte = p.pool.base[r + C::CODES + (b * 16 + tk) * 16 + d % 32 / 2];
-                const float scale = kv4_scale(p.pool.base[r + C::SCALES + (b * 16 + tk) * 2 + 1]);
-                acc[e] += wk * (kv4_value(d & 1 ? byte >> 4 : byte) * scale);
+    }
+
+    // ---- the wavefront's records, up to 64 at a time: lane i holds the (i & 1)-th of its (i / 2)-th step
+    int64_t rec_off = 0;
+    int32_t rec_tok = 0;  // first token; -1: a record that is not there
+    const auto read_records = [&](int32_t first) {  // first: the wavefront's steps before these
+        const int32_t st = step0 + wave + (first + lane / 2) * NW, v = st * 2 + (lane & 1);
+        rec_tok = -1;
+        rec_off = 0;
+        if (st < step1 && v < span.records) {
+            const int32_t rec = v < span.n_sink ? v : v - span.n_sink + span.near;
+            const int32_t page = p.table[(int64_t)at.s * p.max_pages + (rec >> (p.pool.page_shift - 4))];
+            if (page >= 0 && page < p.pool.num_pages) {
+                rec_tok = rec * kKv4Record;
+                rec_off = kv4_record<D>(p.pool, page, g, rec & ((1 << (p.pool.page_shift - 4)) - 1));
             }
         }
+    };
+
+    struct Step {
+        uint32_t k[2][WORDS], v[2][WORDS], scales[2];
+        int32_t tok[2];
+    };
+    // D = 128: a lane takes block kg of token l16, 16 bytes.  D = 64: half kg & 1 of block kg / 2, 8 bytes
+    const int32_t code_off = D == 128 ? lane * 16 : (kg >> 1) * 256 + l16 * 16 + (kg & 1) * 8;
+    const int32_t scale_off = C::SCALES + ((D == 128 ? kg : kg >> 1) * 16 + l16) * 2;
+    const auto fetch = [&](Step &st, int32_t i) {  // the wavefront's i-th step
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int32_t l = (i & 31) * 2 + e;
+            const int64_t off = (int64_t)((uint64_t)(uint32_t)lane_value((int32_t)(rec_off >> 32), l) << 32 | (uint32_t)lane_value((int32_t)rec_off, l));
+            st.tok[e] = lane_value(rec_tok, l);
+            const uint8_t *base = p.pool.base + off;
+            if constexpr (D == 128) {
+                const uint4 k = *reinterpret_cast<const uint4 *>(base + code_off), v = *reinterpret_cast<const uint4 *>(base + C::CODES + code_off);
+                st.k[e][0] = k.x; st.k[e][1] = k.y; st.k[e][2] = k.z; st.k[e][3] = k.w;
+                st.v[e][0] = v.x; st.v[e][1] = v.y; st.v[e][2] = v.z; st.v[e][3] = v.w;
+            } else {
+                const uint2 k = *reinterpret_cast<const uint2 *>(base + code_off), v = *reinterpret_cast<const uint2 *>(base + C::CODES + code_off);
+                st.k[e][0] = k.x; st.k[e][1] = k.y;
+                st.v[e][0] = v.x; st.v[e][1] = v.y;
+            }
+            st.scales[e] = *reinterpret_cast<const uint16_t *>(base + scale_off);
+        }
+    };
+
+    float m_ref = -INFINITY, l_run = 0.f;
+    uint32_t lost = 0;  // 32-element blocks of the pair's output that a NaN block of V reaches
+    f32x4 o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    const auto compute = [&](Step &st) {
+        f32x4 s[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            s[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const float scale = kv4_scale(st.scales[e] & 255u);
+#pragma unroll
+            for (int m = 0; m < KS; ++m) {
+                bf16x2 x[4];
+                kv4_decode8(st.k[e][m], scale, x);
+                const bf16x8 a = {x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[n][m], s[e], 0, 0, 0);
+            }
+        }
+        uint32_t v_scale[2] = {st.scales[0] >> 8, st.scales[1] >> 8};
+        // ---- masks: only where some row does not see some key, or some value is NaN
+        bool whole = true;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            whole = whole && st.tok[e] >= 0 && st.tok[e] + 15 <= pos_lo && (st.tok[e] >= near_hi || st.tok[e] + 15 < r.sink);
+        if (!whole || __any(v_scale[0] == kKv4NanScale || v_scale[1] == kKv4NanScale)) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int32_t tok = st.tok[e];
+                const auto sees = [&](int32_t j) { return tok >= 0 && j <= pos && (j >= near || j < r.sink); };
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!sees(tok + kg * 4 + i)) s[e][i] = -INFINITY;
+                // the values of a key that no row sees, and NaN blocks, count as 0
+                const int32_t mine = tok + l16;
+                const bool seen = tok >= 0 && mine <= pos_hi && (mine >= near_lo || mine < r.sink);
+                for (uint64_t bad = __ballot(seen && v_scale[e] == kKv4NanScale); bad; bad &= bad - 1) {
+                    const int32_t from = __builtin_ctzll(bad);
+                    if (sees(tok + (from & 15))) lost |= 1u << (D == 128 ? from >> 4 : from >> 5);
+                }
+                if (!seen || v_scale[e] == kKv4NanScale) {
+                    v_scale[e] = kKv4Bias;
+#pragma unroll
+                    for (int w = 0; w < WORDS; ++w) st.v[e][w] = 0;
+                }
+            }
+        }
+        // ---- V rows to LDS: chunk c of row t lies at c ^ (t % CH)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float scale = kv4_scale(v_scale[e]);
+            const int32_t t = e * 16 + l16;
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w) {
+                bf16x2 x[4];
+                kv4_decode8(st.v[e][w], scale, x);
+                const uint4 four = make_uint4(__builtin_bit_cast(uint32_t, x[0]), __builtin_bit_cast(uint32_t, x[1]), __builtin_bit_cast(uint32_t, x[2]),
+                                              __builtin_bit_cast(uint32_t, x[3]));
+                *reinterpret_cast<uint4 *>(slice + t * ROWB + (((kg * WORDS + w) ^ (l16 & (CH - 1))) << 4)) = four;
+            }
+        }
+        // ---- weights against the pair's reference, which is raised where a score outgrows it
+        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        if (__any(top * p.c_log2 > m_ref + kStep)) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32)) * p.c_log2;
+            if (top > m_ref + kStep) {
+                const float alpha = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - top);
+                m_ref = top;
+                l_run *= alpha;
+#pragma unroll
+                for (int t = 0; t < DT; ++t) o[t] *= alpha;
+            }
+        }
+        const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+        uint32_t pw[NP][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = i >> 1, j = (i & 1) * 2;
+            const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e][j], p.c_log2, -ref)), b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e][j + 1], p.c_log2, -ref));
+            l_run += a + b;
+            uint32_t part[NP];
+            split_pair<NP>(a, b, part);
+#pragma unroll
+            for (int n = 0; n < NP; ++n) pw[n][i] = part[n];
+        }
+        // ---- O^T += V^T P^T: k index kg * 8 + j is token kg * 4 + j of the first record, j < 4, or + j - 4 of the second
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            bf16x8 a;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int32_t tr = kg * 4 + (l16 >> 2);
+                const uint8_t *src = slice + (e * 16 + tr) * ROWB + (((t * 2 + ((l16 & 3) >> 1)) ^ (tr & (CH - 1))) << 4) + (l16 & 1) * 8;
+                const bf16x4 four = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, src)));
+                a[e * 4] = four[0]; a[e * 4 + 1] = four[1]; a[e * 4 + 2] = four[2]; a[e * 4 + 3] = four[3];
+            }
+#pragma unroll
+            for (int n = 0; n < NP; ++n) {
+                const uint4 b = make_uint4(pw[n][0], pw[n][1], pw[n][2], pw[n][3]);
+                o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, b), o[t], 0, 0, 0);
+            }
+        }
+    };
+
+    const int32_t mine = step1 - step0 > wave ? (step1 - step0 - wave + NW - 1) / NW : 0;  // the wavefront's steps
+    if (mine > 0) {
+        Step now, next;
+        read_records(0);
+        fetch(now, 0);
+        for (int32_t i = 0; i < mine; ++i) {
+            if (i + 1 < mine) {
+                if (((i + 1) & 31) == 0) read_records(i + 1);
+                fetch(next, i + 1);
+            }
+            compute(now);
+            now = next;
+        }
     }
-    const bool none = m == -INFINITY && l == 0.f;
-    for (int e = 0; e < D / 64; ++e) {
-        const float x = none ? 0.f : acc[e] / l;
-        const int64_t o = ((int64_t)row * p.n_q_heads + h) * D + lane * (D / 64) + e;
-        if (BF16) ((uint16_t *)p.out)[o] = bf16_nearest(x);
-        else ((float *)p.out)[o] = x;
+
+    // ---- the wavefronts' parts of a pair: O^T to the wavefronts' slices as [pair][D] (each has 16 * D * 4 bytes), joined by all
+    l_run += __shfl_xor(l_run, 16);
+    l_run += __shfl_xor(l_run, 32);
+    float *const mine_o = reinterpret_cast<float *>(slice);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+        if (lost >> (t >> 1) & 1u) o[t] = f32x4{NAN, NAN, NAN, NAN};
+        *reinterpret_cast<f32x4 *>(mine_o + l16 * D + t * 16 + kg * 4) = o[t];
     }
-    if (p.lse && lane == 0) p.lse[(int64_t)row * p.n_q_heads + h] = none ? -INFINITY : m + logf(l);
+    if (kg == 0) {
+        lds_ml[wave][l16][0] = m_ref;
+        lds_ml[wave][l16][1] = l_run;
+    }
+    __syncthreads();
+    const float *const all_o = reinterpret_cast<const float *>(lds);
+    for (int32_t i = tid; i < n_pairs * (D / 4); i += NW * 64) {
+        const int32_t pr = i / (D / 4), d4 = i % (D / 4) * 4;
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, lds_ml[w][pr][0]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        float l = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = __builtin_amdgcn_exp2f(lds_ml[w][pr][0] - ref);
+            l += f * lds_ml[w][pr][1];
+            acc += f * *reinterpret_cast<const f32x4 *>(all_o + (w * kKv4Pairs + pr) * D + d4);
+        }
+        if (at.splits > 1) {
+            const int64_t slot = (int64_t)item * kKv4Pairs + pr;
+            *reinterpret_cast<f32x4 *>(p.part_acc + slot * D + d4) = acc;
+            if (d4 == 0) {
+                p.part_ml[slot * 2] = M;
+                p.part_ml[slot * 2 + 1] = l;
+            }
+        } else {
+            const int32_t pp = pair0 + pr, rr = pp / G, hh = p.heads.order[head0 + pp - rr * G];
+            const int64_t to = ((int64_t)(r.row0 + rr) * p.n_q_heads + hh);
+            const bool none = M == -INFINITY && l == 0.f;
+            const float inv = none ? 0.f : 1.f / l;
+            if (none) acc = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (BF16) {
+                const ushort4 x = make_ushort4(bf16_nearest(acc[0] * inv), bf16_nearest(acc[1] * inv), bf16_nearest(acc[2] * inv), bf16_nearest(acc[3] * inv));
+                *reinterpret_cast<ushort4 *>((uint16_t *)p.out + to * D + d4) = x;
+            } else {
+                *reinterpret_cast<f32x4 *>((float *)p.out + to * D + d4) = acc * inv;
+            }
+            if (p.lse && d4 == 0) p.lse[to] = none ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        }
+    }
 }
 
-hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, hipStream_t stream)
+// Joins the items of the units that were cut: a workgroup of D / 4 lanes takes a pair
+template <int D, bool BF16>
+__global__ __launch_bounds__(64) void merge_kv4_kernel(Kv4Attn p, int32_t pairs_of_unit)
+{
+    const int32_t unit = blockIdx.x / pairs_of_unit, pr = blockIdx.x % pairs_of_unit, lane = threadIdx.x;
+    const Place at = find_place<true>(p, unit, false);
+    if (at.s < 0 || at.splits < 2) return;
+    const int32_t tile = at.rest % at.tiles, g = at.rest / at.tiles;
+    const int32_t head0 = p.heads.first[g], G = p.heads.first[g + 1] - head0;
+    const int32_t pair = tile * kKv4Pairs + pr;
+    if (pair >= at.r.rows * G) return;
+    const int64_t item0 = at.first_item + ((int64_t)g * at.splits) * at.tiles + tile;
+    if (item0 + (int64_t)(at.splits - 1) * at.tiles >= p.max_items) return;
+    float M = -INFINITY;
+    for (int32_t s = lane; s < at.splits; s += 64) M = fmaxf(M, p.part_ml[((item0 + (int64_t)s * at.tiles) * kKv4Pairs + pr) * 2]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    const float ref = M == -INFINITY ? 0.f : M;
+    constexpr int LPR = D / 4, NSUB = 64 / LPR;
+    const int32_t sub = lane / LPR, d4 = lane % LPR * 4;
+    float l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int32_t s = sub; s < at.splits; s += NSUB) {
+        const int64_t slot = (item0 + (int64_t)s * at.tiles) * kKv4Pairs + pr;
+        const float f = __builtin_amdgcn_exp2f(p.part_ml[slot * 2] - ref);
+        l += f * p.part_ml[slot * 2 + 1];
+        acc += f * *reinterpret_cast<const f32x4 *>(p.part_acc + slot * D + d4);
+    }
+#pragma unroll
+    for (int o = LPR; o < 64; o <<= 1) {
+        l += __shfl_xor(l, o);
+        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], o);
+    }
+    if (sub != 0) return;
+    const int32_t row = pair / G, head = p.heads.order[head0 + pair - row * G];
+    const int64_t to = (int64_t)(at.r.row0 + row) * p.n_q_heads + head;
+    const bool none = M == -INFINITY && l == 0.f;
+    const float inv = none ? 0.f : 1.f / l;
+    if (none) acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (BF16) {
+        const ushort4 x = make_ushort4(bf16_nearest(acc[0] * inv), bf16_nearest(acc[1] * inv), bf16_nearest(acc[2] * inv), bf16_nearest(acc[3] * inv));
+        *reinterpret_cast<ushort4 *>((uint16_t *)p.out + to * D + d4) = x;
+    } else {
+        *reinterpret_cast<f32x4 *>((float *)p.out + to * D + d4) = acc * inv;
+    }
+    if (p.lse && d4 == 0) p.lse[to] = none ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, bool merge, hipStream_t stream)
 {
     const auto kernel = D == 128 ? (bf16 ? attn_kv4_kernel<128, true> : attn_kv4_kernel<128, false>)
                                  : (bf16 ? attn_kv4_kernel<64, true> : attn_kv4_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, dim3(p.num_rows, p.n_q_heads), dim3(64), 0, stream, p);
+    hipLaunchKernelGGL(kernel, dim3((p.max_items + 7) / 8 * 8), dim3(NW * 64), 0, stream, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !merge) return e;
+    const int32_t pairs = (int32_t)((int64_t)p.num_rows * p.group < kKv4Pairs ? p.num_rows * p.group : kKv4Pairs);
+    const auto join = D == 128 ? (bf16 ? merge_kv4_kernel<128, true> : merge_kv4_kernel<128, false>)
+                               : (bf16 ? merge_kv4_kernel<64, true> : merge_kv4_kernel<64, false>);
+    hipLaunchKernelGGL(join, dim3(p.max_units * pairs), dim3(64), 0, stream, p, pairs);
     return hipGetLastError();
 }
 

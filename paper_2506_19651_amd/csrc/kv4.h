@@ -31,18 +31,18 @@ __host__ __device__ inline int64_t kv4_record(const Kv4Pool &p, int32_t page, in
 // 2^e as a float, -126 <= e <= 127
 __device__ __forceinline__ float exp2_int(int32_t e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// Scale of a block from its byte; bytes that no store writes give what they say, 0 the nearest normal number
-__device__ __forceinline__ float kv4_scale(uint32_t byte)
-{
-    return __uint_as_float(byte == kKv4NanScale ? 0x7fc00000u : (byte ? byte : 1u) << 23);
-}
+// A block's scale from its byte, as the conversion instructions take it: they read the exponent only, and make NaN of 255
+__device__ __forceinline__ float kv4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-__device__ __forceinline__ float kv4_value(uint32_t code)  // of the low four bits
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+// The eight values of a word of codes, in order, as bf16: exact
+__device__ __forceinline__ void kv4_decode8(uint32_t codes, float scale, bf16x2 (&x)[4])
 {
-    const uint32_t m = code & 7u;
-    // 0, 1/2: m / 2; from 1 on one mantissa bit under an exponent
-    const float x = m < 2 ? 0.5f * m : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
-    return code & 8u ? -x : x;
+    x[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+    x[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+    x[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+    x[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
 }
 
 struct Kv4Slots {
@@ -60,20 +60,35 @@ struct Kv4Rows {  // rows of K and V that go into slots, or come out of them
     Kv4Pool pool;
 };
 
+// Attention.  A KV head's (row, query head) pairs of a request, head fastest, are cut into tiles of kKv4Pairs; a unit is one tile
+// against all keys that the request's rows see, in steps of kKv4Step tokens.  Units are cut into items of about equal
+// length: a workgroup takes an item.
+constexpr int32_t kKv4Pairs = 16;
+constexpr int32_t kKv4Step = 32;
+
+struct Kv4Heads {
+    uint8_t order[kMaxHeads];         // query heads sorted by KV head
+    uint16_t first[kMaxHeads + 1];    // KV head g's are order[first[g] .. first[g + 1])
+};
+
 struct Kv4Attn {
     const void *q;
     void *out;
     float *lse;
     Kv4Pool pool;
     const int32_t *table, *row_start, *row_len, *seq_len, *sink_len, *window;
+    float *part_acc, *part_ml;        // [item][kKv4Pairs][D], [item][kKv4Pairs][2]: of items that are not whole units
     int32_t num_seqs, max_pages, num_rows, n_q_heads;
-    float scale;
-    HeadTable heads;
+    int32_t group;                    // query heads of the KV head that has most
+    int32_t target_items, min_steps;  // items that a call is cut into, if they are not shorter than this
+    int32_t max_items, max_units;     // bounds that no lengths pass
+    float c_log2;                     // softmax scale * log2(e)
+    Kv4Heads heads;
 };
 
 hipError_t launch_kv4_slots(const Kv4Slots &p, hipStream_t stream);
 hipError_t launch_kv4_store(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream);
 hipError_t launch_kv4_load(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream);
-hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, hipStream_t stream);
+hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, bool merge, hipStream_t stream);
 
 }  // namespace pevlm

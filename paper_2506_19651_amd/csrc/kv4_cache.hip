@@ -186,10 +186,17 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows p)
     const uint32_t w[4] = {c.x, c.y, c.z, c.w};
     const int64_t to = (int64_t)row * (which ? p.v_stride : p.k_stride) + head * D + b * 32;
     void *dst = which ? p.v : p.k;
-    for (int i = 0; i < 32; ++i) {
-        const float x = kv4_value(w[i / 8] >> (i % 8 * 4)) * scale;
-        if (BF16) ((uint16_t *)dst)[to + i] = (uint16_t)(__float_as_uint(x) >> 16);  // exact: two significant bits
-        else ((float *)dst)[to + i] = x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bf16x2 x[4];
+        kv4_decode8(w[i], scale, x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t two = __builtin_bit_cast(uint32_t, x[j]);  // exact: a value has two significant bits
+            const int64_t at = to + i * 8 + j * 2;
+            if (BF16) *reinterpret_cast<uint32_t *>((uint16_t *)dst + at) = two;
+            else *reinterpret_cast<float2 *>((float *)dst + at) = make_float2(__uint_as_float(two << 16), __uint_as_float(two & 0xffff0000u));
+        }
     }
 }
 
