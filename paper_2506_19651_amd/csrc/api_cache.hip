@@ -90,10 +90,13 @@ static void size_attn(const pevlm_heads *h, int32_t num_seqs, int32_t num_rows, 
     p->group = group_heads(tab, h, &p->heads);
     const int64_t asking = std::min(num_seqs, num_rows);
     const int64_t units = h->n_kv_heads * (asking + (int64_t)num_rows * p->group / kKv4Pairs);
-    p->target_items = 2 * compute_units();
-    p->min_steps = 16;
+    const int32_t target = 6 * compute_units();
+    p->target_rcp = 1.f / (float)target;
+    p->min_steps = 12;
+    p->mapped = h->kv_head_of_q != nullptr;
+    p->by_xcd = p->group > kKv4Pairs || (int64_t)num_rows * p->group > (int64_t)kKv4Pairs * num_seqs;
     p->max_units = (int32_t)std::min<int64_t>(units, INT32_MAX);
-    p->max_items = (int32_t)std::min<int64_t>(units + p->target_items, INT32_MAX);
+    p->max_items = (int32_t)std::min<int64_t>(units + target + 8, INT32_MAX);
 }
 
 static size_t ml_bytes(const Kv4Attn &p) { return align256((size_t)p.max_items * kKv4Pairs * 2 * sizeof(float)); }
@@ -221,11 +224,12 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
     p.num_rows = num_rows;
     p.n_q_heads = heads->n_q_heads;
     p.part_ml = (float *)workspace;
+    // no request is longer than its row of the table
+    const int64_t longest = ceil_div(ceil_div(cache->max_pages * cache->page_size, kKv4Step), p.min_steps);
+    p.grid = (int32_t)std::min<int64_t>(p.max_items, p.max_units * longest);
     p.part_acc = (float *)((char *)workspace + ml_bytes(p));
     p.c_log2 = scale_of(heads) * 1.4426950408889634f;
-    // a table too short for a second item of a unit leaves nothing to merge
-    const bool merge = (int64_t)cache->max_pages * cache->page_size > (int64_t)p.min_steps * kKv4Step;
-    const hipError_t e = launch_attn_kv4(p, heads->head_dim, heads->dtype == PEVLM_BF16, merge, (hipStream_t)stream);
+    const hipError_t e = launch_attn_kv4(p, heads->head_dim, heads->dtype == PEVLM_BF16, longest > 1, (hipStream_t)stream);
     return e == hipSuccess ? PEVLM_OK : hip_fail(e, "cache attention launch");
 }
 

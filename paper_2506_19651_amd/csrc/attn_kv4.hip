@@ -11,12 +11,14 @@
 // parts (fp32); products of parts are exact in fp32, sums are fp32 throughout.
 #include "bf16_device.h"
 #include "kv4.h"
+#include "wave_scan.h"
 
 namespace pevlm {
 
 namespace {
 
-constexpr int NW = 8;  // wavefronts of a workgroup
+constexpr int NW = 4;  // wavefronts of a workgroup
+constexpr int AHEAD = 1;  // steps whose loads are under way before the one at hand
 constexpr int32_t kMany = 0x3fffffff;
 
 // What a request's rows see: records (16 tokens) [0, n_sink) and [near, near + n_near), which do not overlap
@@ -65,14 +67,9 @@ __device__ __forceinline__ Span span_of(const Request &r)
 
 __device__ __forceinline__ int32_t steps_of(const Span &s) { return ceil_div(s.records, kKv4Step / kKv4Record); }
 
-__device__ __forceinline__ int64_t wave_sum(int64_t x)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    return x;
-}
-
 __device__ __forceinline__ int32_t lane_value(int32_t x, int32_t lane) { return __builtin_amdgcn_readlane(x, lane); }
+// a value that is the same in every lane, where the compiler is to know it
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // Where the idx-th item (or unit) of a call lies.  Every wavefront finds its own by itself: lane by lane over 64 requests at a
 // time, once for the whole work, which sets the items' length, and once for the place.
@@ -82,10 +79,9 @@ struct Place {
 };
 
 template <bool UNITS>
-__device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx_of_xcd, bool by_xcd)
+__device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
 {
     const int32_t lane = threadIdx.x & 63;
-    int64_t work = 0;
     Request r;
     int32_t steps = 0, tiles = 0;
     const auto look = [&](int32_t s) {
@@ -93,55 +89,46 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx_of_xcd
         if (s < p.num_seqs) {
             r = read_request(p, s);
             if (r.rows > 0) {
-                tiles = (int32_t)(((int64_t)r.rows * p.group + kKv4Pairs - 1) / kKv4Pairs);
+                tiles = r.rows * p.group <= kKv4Pairs ? 1 : (int32_t)(((int64_t)r.rows * p.group + kKv4Pairs - 1) / kKv4Pairs);
                 steps = steps_of(span_of(r));
             }
         }
     };
-    for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
-        look(s0 + lane);
-        work += (int64_t)tiles * steps;
-    }
-    work = wave_sum(work) * p.pool.n_kv_heads;
-    int64_t length = (work + p.target_items - 1) / p.target_items;  // steps of an item
-    length = length > p.min_steps ? length : p.min_steps;
-    const int32_t per = (int32_t)(length < INT32_MAX ? length : INT32_MAX);
-
     // Counts stop at kMany: with row ranges that overlap they can pass any bound, and no item or unit lies there
     const auto count = [&](int32_t n) {
         const int64_t x = (int64_t)n * tiles * p.pool.n_kv_heads;
         return (int32_t)(x < kMany ? x : kMany);
     };
     const auto sum = [](int32_t a, int32_t b) { return a + b < kMany ? a + b : kMany; };
+    const auto total = [](auto x) { return __builtin_bit_cast(decltype(x), lane_value(__builtin_bit_cast(int32_t, x), 63)); };
+    float work = 0.f;  // what it rounds off moves the items' length by less than one part in 2^18, and max_items has room for that
+    for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
+        look(s0 + lane);
+        work += total(wave_scan((float)steps * (float)tiles, [](float a, float b) { return a + b; }));
+    }
+    const float length = work * (float)p.pool.n_kv_heads * p.target_rcp;  // steps of an item
+    const int32_t per = length < (float)p.min_steps ? p.min_steps : (length < 1e9f ? (int32_t)length + 1 : 1000000000);
+    const auto splits_of = [&] { return steps > per ? ceil_div(steps, per) : 1; };  // rows that see nothing are an item, too
+
     Place at;
     at.s = -1;
     at.first_item = 0;
-    int32_t before = 0;
-    int32_t idx = idx_of_xcd;
-    if (by_xcd) {  // all items, to deal contiguous eighths of them to the XCDs
-        int64_t items = 0;
+    if (!UNITS && p.by_xcd) {  // contiguous eighths of the items to the XCDs
+        int32_t all = 0;
         for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
             if (p.num_seqs > 64) look(s0 + lane);
-            items += count(steps ? ceil_div(steps, per) : 1);
+            all = sum(all, total(wave_scan(count(splits_of()), sum)));
         }
-        items = wave_sum(items);
-        const int32_t all = (int32_t)(items < p.max_items ? items : p.max_items), per_xcd = (all + 7) / 8;
-        idx = (idx & 7) * per_xcd + (idx >> 3);
-        if (idx_of_xcd >> 3 >= per_xcd || idx >= all) return at;
+        all = all < p.max_items ? all : p.max_items;
+        const int32_t per_xcd = (all + 7) / 8, j = idx >> 3;
+        idx = (idx & 7) * per_xcd + j;
+        if (j >= per_xcd || idx >= all) return at;
     }
+    int32_t before = 0;
     for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
         if (p.num_seqs > 64) look(s0 + lane);
-        const int32_t splits = steps ? ceil_div(steps, per) : 1;  // rows that see nothing are an item, too
-        const int32_t items = count(splits), mine = UNITS ? count(1) : items;
-        int32_t end = mine, item_end = items;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int32_t y = __shfl_up(end, o), z = __shfl_up(item_end, o);
-            if (lane >= o) {
-                end = sum(end, y);
-                item_end = sum(item_end, z);
-            }
-        }
+        const int32_t splits = splits_of(), items = count(splits), mine = UNITS ? count(1) : items;
+        const int32_t end = wave_scan(mine, sum), item_end = UNITS ? wave_scan(items, sum) : end;
         const uint64_t found = __ballot(sum(before, end) > idx);
         if (found) {
             const int32_t f = __builtin_ctzll(found);
@@ -157,11 +144,28 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx_of_xcd
             at.r.window = lane_value(r.window, f);
             return at;
         }
-        before = sum(before, lane_value(end, 63));
-        at.first_item = sum(at.first_item, lane_value(item_end, 63));
+        before = sum(before, total(end));
+        at.first_item = sum(at.first_item, total(item_end));
     }
     return at;
 }
+
+// x / d and the rest of it
+__device__ __forceinline__ int32_t divide(int32_t x, int32_t d, int32_t &rest)
+{
+    if (d == 1) {
+        rest = 0;
+        return x;
+    }
+    const int32_t n = x / d;
+    rest = x - n * d;
+    return n;
+}
+
+// A KV head's query heads: as a map sorts them, or equal groups in order
+__device__ __forceinline__ int32_t first_head(const Kv4Attn &p, int32_t g) { return p.mapped ? p.heads.first[g] : g * p.group; }
+__device__ __forceinline__ int32_t heads_of(const Kv4Attn &p, int32_t g) { return p.mapped ? p.heads.first[g + 1] - p.heads.first[g] : p.group; }
+__device__ __forceinline__ int32_t query_head(const Kv4Attn &p, int32_t i) { return p.mapped ? p.heads.order[i] : i; }
 
 __device__ __forceinline__ uint16_t bf16_nearest(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 
@@ -180,12 +184,27 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&part)[N]
     }
 }
 
+// Four elements of a pair's row, from the values and sum of its weights against reference M
+template <int D, bool BF16>
+__device__ __forceinline__ void store_pair(const Kv4Attn &p, int64_t to, int32_t d4, f32x4 acc, float M, float l)
+{
+    const bool none = M == -INFINITY && l == 0.f;  // a row that sees nothing
+    acc = none ? f32x4{0.f, 0.f, 0.f, 0.f} : acc * (1.f / l);
+    if constexpr (BF16) {
+        const ushort4 x = make_ushort4(bf16_nearest(acc[0]), bf16_nearest(acc[1]), bf16_nearest(acc[2]), bf16_nearest(acc[3]));
+        *reinterpret_cast<ushort4 *>((uint16_t *)p.out + to * D + d4) = x;
+    } else {
+        *reinterpret_cast<f32x4 *>((float *)p.out + to * D + d4) = acc;
+    }
+    if (p.lse && d4 == 0) p.lse[to] = none ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
 constexpr float kStep = 8.f;  // base-2 units that a row's maximum may outgrow its reference by
 
 }  // namespace
 
 template <int D, bool BF16>
-__global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
+__global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_kernel(Kv4Attn p)
 {
     using C = Kv4Cfg<D>;
     constexpr int KS = D / 32;         // k-steps of a score
@@ -198,17 +217,18 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
     __shared__ __attribute__((aligned(1024))) uint8_t lds[NW * 32 * ROWB];
     __shared__ float lds_ml[NW][kKv4Pairs][2];
 
-    const Place at = find_place<false>(p, blockIdx.x, true);
+    const Place at = find_place<false>(p, blockIdx.x);
     if (at.s < 0) return;
     const Request r = at.r;
-    const int32_t tile = at.rest % at.tiles, split = at.rest / at.tiles % at.splits, g = at.rest / (at.tiles * at.splits);
+    int32_t tile, split;
+    const int32_t g = divide(divide(at.rest, at.tiles, tile), at.splits, split);
     const int32_t item = at.first_item + at.rest;
-    const int32_t head0 = p.heads.first[g], G = p.heads.first[g + 1] - head0;
+    const int32_t head0 = first_head(p, g), G = heads_of(p, g);
     const int32_t pair0 = tile * kKv4Pairs, n_pairs_all = r.rows * G;
     const int32_t n_pairs = n_pairs_all - pair0 < kKv4Pairs ? n_pairs_all - pair0 : kKv4Pairs;
     if (n_pairs <= 0) return;
     const Span span = span_of(r);
-    const int32_t steps = steps_of(span), per = ceil_div(steps, at.splits);
+    const int32_t steps = steps_of(span), per = at.splits == 1 ? steps : ceil_div(steps, at.splits);
     const int32_t step0 = split * per, step1 = step0 + per < steps ? step0 + per : steps;
 
     const int32_t tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, kg = lane >> 4;
@@ -217,7 +237,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
 
     // this lane's pair (column of S^T)
     const int32_t pair = pair0 + (l16 < n_pairs ? l16 : n_pairs - 1);
-    const int32_t row = pair / G, head = p.heads.order[head0 + pair - row * G];
+    const int32_t row = pair / G, head = query_head(p, head0 + pair - row * G);
     const int32_t pos = r.held - r.rows + row, near = near_of(r, pos);
     // the tile's first and last rows: positions and windows rise with the row
     const int32_t pos_lo = r.held - r.rows + pair0 / G, pos_hi = r.held - r.rows + (pair0 + n_pairs - 1) / G;
@@ -248,19 +268,23 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
         }
     }
 
-    // ---- the wavefront's records, up to 64 at a time: lane i holds the (i & 1)-th of its (i / 2)-th step
-    int64_t rec_off = 0;
-    int32_t rec_tok = 0;  // first token; -1: a record that is not there
+    // ---- the wavefront's records, 64 steps at a time: lane i holds those of step i of them
+    int64_t rec_off[2];
+    int32_t rec_tok[2];  // first token; -1: a record that is not there
     const auto read_records = [&](int32_t first) {  // first: the wavefront's steps before these
-        const int32_t st = step0 + wave + (first + lane / 2) * NW, v = st * 2 + (lane & 1);
-        rec_tok = -1;
-        rec_off = 0;
-        if (st < step1 && v < span.records) {
-            const int32_t rec = v < span.n_sink ? v : v - span.n_sink + span.near;
-            const int32_t page = p.table[(int64_t)at.s * p.max_pages + (rec >> (p.pool.page_shift - 4))];
-            if (page >= 0 && page < p.pool.num_pages) {
-                rec_tok = rec * kKv4Record;
-                rec_off = kv4_record<D>(p.pool, page, g, rec & ((1 << (p.pool.page_shift - 4)) - 1));
+        const int32_t st = step0 + wave + (first + lane) * NW;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int32_t v = st * 2 + e;
+            rec_tok[e] = -1;
+            rec_off[e] = 0;
+            if (st < step1 && v < span.records) {
+                const int32_t rec = v < span.n_sink ? v : v - span.n_sink + span.near;
+                const int32_t page = p.table[(int64_t)at.s * p.max_pages + (rec >> (p.pool.page_shift - 4))];
+                if (page >= 0 && page < p.pool.num_pages) {
+                    rec_tok[e] = rec * kKv4Record;
+                    rec_off[e] = kv4_record<D>(p.pool, page, g, rec & ((1 << (p.pool.page_shift - 4)) - 1));
+                }
             }
         }
     };
@@ -270,14 +294,14 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
         int32_t tok[2];
     };
     // D = 128: a lane takes block kg of token l16, 16 bytes.  D = 64: half kg & 1 of block kg / 2, 8 bytes
-    const int32_t code_off = D == 128 ? lane * 16 : (kg >> 1) * 256 + l16 * 16 + (kg & 1) * 8;
-    const int32_t scale_off = C::SCALES + ((D == 128 ? kg : kg >> 1) * 16 + l16) * 2;
-    const auto fetch = [&](Step &st, int32_t i) {  // the wavefront's i-th step
+    const uint32_t code_off = D == 128 ? lane * 16 : (kg >> 1) * 256 + l16 * 16 + (kg & 1) * 8;
+    // the two scale bytes lie in one half of a word (loads of two bytes are widened where they arrive, in front of their use)
+    const uint32_t scale_off = C::SCALES + ((D == 128 ? kg : kg >> 1) * 16 + (l16 & 14)) * 2, scale_bit = (l16 & 1) * 16;
+    const auto fetch = [&](Step &st, int32_t i) {  // the i-th of those steps
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int32_t l = (i & 31) * 2 + e;
-            const int64_t off = (int64_t)((uint64_t)(uint32_t)lane_value((int32_t)(rec_off >> 32), l) << 32 | (uint32_t)lane_value((int32_t)rec_off, l));
-            st.tok[e] = lane_value(rec_tok, l);
+            const int64_t off = (int64_t)((uint64_t)(uint32_t)lane_value((int32_t)(rec_off[e] >> 32), i) << 32 | (uint32_t)lane_value((int32_t)rec_off[e], i));
+            st.tok[e] = lane_value(rec_tok[e], i);
             const uint8_t *base = p.pool.base + off;
             if constexpr (D == 128) {
                 const uint4 k = *reinterpret_cast<const uint4 *>(base + code_off), v = *reinterpret_cast<const uint4 *>(base + C::CODES + code_off);
@@ -288,7 +312,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
                 st.k[e][0] = k.x; st.k[e][1] = k.y;
                 st.v[e][0] = v.x; st.v[e][1] = v.y;
             }
-            st.scales[e] = *reinterpret_cast<const uint16_t *>(base + scale_off);
+            st.scales[e] = *reinterpret_cast<const uint32_t *>(base + scale_off);
         }
     };
 
@@ -303,7 +327,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             s[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const float scale = kv4_scale(st.scales[e] & 255u);
+            const float scale = kv4_scale(st.scales[e] >> scale_bit & 255u);
 #pragma unroll
             for (int m = 0; m < KS; ++m) {
                 bf16x2 x[4];
@@ -313,7 +337,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
                 for (int n = 0; n < NQ; ++n) s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[n][m], s[e], 0, 0, 0);
             }
         }
-        uint32_t v_scale[2] = {st.scales[0] >> 8, st.scales[1] >> 8};
+        uint32_t v_scale[2] = {st.scales[0] >> (scale_bit + 8) & 255u, st.scales[1] >> (scale_bit + 8) & 255u};
         // ---- masks: only where some row does not see some key, or some value is NaN
         bool whole = true;
 #pragma unroll
@@ -399,18 +423,23 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
         }
     };
 
+    // Loads go out AHEAD steps in front of the one at hand, on every step (behind the last the last one's again): a load under a
+    // condition makes the compiler wait for all of them where the paths meet.
     const int32_t mine = step1 - step0 > wave ? (step1 - step0 - wave + NW - 1) / NW : 0;  // the wavefront's steps
-    if (mine > 0) {
-        Step now, next;
-        read_records(0);
-        fetch(now, 0);
-        for (int32_t i = 0; i < mine; ++i) {
-            if (i + 1 < mine) {
-                if (((i + 1) & 31) == 0) read_records(i + 1);
-                fetch(next, i + 1);
+    for (int32_t first = 0; first < mine; first += 64) {
+        const int32_t n = mine - first < 64 ? mine - first : 64;
+        Step st[AHEAD + 1];
+        read_records(first);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) fetch(st[u], u < n ? u : n - 1);
+        for (int32_t i = 0; i < n; i += AHEAD + 1) {
+#pragma unroll
+            for (int u = 0; u <= AHEAD; ++u) {
+                if (i + u >= n) break;
+                const int32_t ahead = i + u + AHEAD;
+                fetch(st[(u + AHEAD) % (AHEAD + 1)], ahead < n ? ahead : n - 1);
+                compute(st[u]);
             }
-            compute(now);
-            now = next;
         }
     }
 
@@ -451,81 +480,106 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_kernel(Kv4Attn p)
                 p.part_ml[slot * 2 + 1] = l;
             }
         } else {
-            const int32_t pp = pair0 + pr, rr = pp / G, hh = p.heads.order[head0 + pp - rr * G];
-            const int64_t to = ((int64_t)(r.row0 + rr) * p.n_q_heads + hh);
-            const bool none = M == -INFINITY && l == 0.f;
-            const float inv = none ? 0.f : 1.f / l;
-            if (none) acc = f32x4{0.f, 0.f, 0.f, 0.f};
-            if constexpr (BF16) {
-                const ushort4 x = make_ushort4(bf16_nearest(acc[0] * inv), bf16_nearest(acc[1] * inv), bf16_nearest(acc[2] * inv), bf16_nearest(acc[3] * inv));
-                *reinterpret_cast<ushort4 *>((uint16_t *)p.out + to * D + d4) = x;
-            } else {
-                *reinterpret_cast<f32x4 *>((float *)p.out + to * D + d4) = acc * inv;
-            }
-            if (p.lse && d4 == 0) p.lse[to] = none ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+            const int32_t pp = pair0 + pr, rr = pp / G, hh = query_head(p, head0 + pp - rr * G);
+            store_pair<D, BF16>(p, (int64_t)(r.row0 + rr) * p.n_q_heads + hh, d4, acc, M, l);
         }
     }
 }
 
-// Joins the items of the units that were cut: a workgroup of D / 4 lanes takes a pair
-template <int D, bool BF16>
-__global__ __launch_bounds__(64) void merge_kv4_kernel(Kv4Attn p, int32_t pairs_of_unit)
+// Joins the items of the units that were cut.  WAVES wavefronts take a pair, a workgroup of 256 or more lanes one or two pairs of a unit:
+// D / 4 lanes cover a row of values and the groups of them take the items in turn, kTurn at once with their maxima and sums, against a
+// running maximum of their own; then the groups are joined.  A lane that walks all items takes a memory round trip for each (23 us for 128 items
+// of 28 pairs), and to fetch all maxima before the first values is one round trip more.
+constexpr int kTurn = 6;
+
+template <int D, bool BF16, int WAVES>
+__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void merge_kv4_kernel(Kv4Attn p, int32_t pairs_of_unit)
 {
-    const int32_t unit = blockIdx.x / pairs_of_unit, pr = blockIdx.x % pairs_of_unit, lane = threadIdx.x;
-    const Place at = find_place<true>(p, unit, false);
+    constexpr int LPR = D / 4, NSUB = WAVES * 64 / LPR, PAIRS = WAVES == 16 ? 1 : 4 / WAVES;
+    __shared__ float parts[PAIRS][NSUB][D], ml[PAIRS][NSUB][2];
+    int32_t pr;
+    const int32_t unit = divide(blockIdx.x, ceil_div(pairs_of_unit, PAIRS), pr);
+    const Place at = find_place<true>(p, unit);
     if (at.s < 0 || at.splits < 2) return;
-    const int32_t tile = at.rest % at.tiles, g = at.rest / at.tiles;
-    const int32_t head0 = p.heads.first[g], G = p.heads.first[g + 1] - head0;
-    const int32_t pair = tile * kKv4Pairs + pr;
-    if (pair >= at.r.rows * G) return;
+    int32_t tile;
+    const int32_t g = divide(at.rest, at.tiles, tile);
+    const int32_t head0 = first_head(p, g), G = heads_of(p, g);
+    const int32_t n_pairs = at.r.rows * G - tile * kKv4Pairs;  // left in this tile and behind it
+    if (pr * PAIRS >= n_pairs || pr * PAIRS >= kKv4Pairs) return;
     const int64_t item0 = at.first_item + ((int64_t)g * at.splits) * at.tiles + tile;
     if (item0 + (int64_t)(at.splits - 1) * at.tiles >= p.max_items) return;
-    float M = -INFINITY;
-    for (int32_t s = lane; s < at.splits; s += 64) M = fmaxf(M, p.part_ml[((item0 + (int64_t)s * at.tiles) * kKv4Pairs + pr) * 2]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    const float ref = M == -INFINITY ? 0.f : M;
-    constexpr int LPR = D / 4, NSUB = 64 / LPR;
-    const int32_t sub = lane / LPR, d4 = lane % LPR * 4;
-    float l = 0.f;
+    const int32_t mine = __builtin_amdgcn_readfirstlane(threadIdx.x / (WAVES * 64)), tid = threadIdx.x % (WAVES * 64);
+    const int32_t in_tile = pr * PAIRS + mine, pair = tile * kKv4Pairs + in_tile;
+    const int64_t slot0 = item0 * kKv4Pairs + in_tile, stride = (int64_t)at.tiles * kKv4Pairs;
+    const int32_t sub = tid / LPR, d4 = tid % LPR * 4;
+    float M = -INFINITY, l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int32_t s = sub; s < at.splits; s += NSUB) {
-        const int64_t slot = (item0 + (int64_t)s * at.tiles) * kKv4Pairs + pr;
-        const float f = __builtin_amdgcn_exp2f(p.part_ml[slot * 2] - ref);
-        l += f * p.part_ml[slot * 2 + 1];
-        acc += f * *reinterpret_cast<const f32x4 *>(p.part_acc + slot * D + d4);
-    }
+    for (int32_t s0 = sub; s0 < at.splits; s0 += NSUB * kTurn) {
+        f32x4 a[kTurn];
+        float2 v[kTurn];
 #pragma unroll
-    for (int o = LPR; o < 64; o <<= 1) {
-        l += __shfl_xor(l, o);
-        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], o);
+        for (int u = 0; u < kTurn; ++u) {
+            const int32_t s = s0 + u * NSUB;
+            const int64_t slot = slot0 + (s < at.splits ? s : s0) * stride;
+            a[u] = *reinterpret_cast<const f32x4 *>(p.part_acc + slot * D + d4);
+            v[u] = *reinterpret_cast<const float2 *>(p.part_ml + slot * 2);
+        }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < kTurn; ++u) top = fmaxf(top, v[u].x);
+        const float ref = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(M - ref);
+        l *= old;
+        acc *= old;
+        M = top;
+#pragma unroll
+        for (int u = 0; u < kTurn; ++u)
+            if (s0 + u * NSUB < at.splits) {
+                const float f = __builtin_amdgcn_exp2f(v[u].x - ref);
+                l += f * v[u].y;
+                acc += f * a[u];
+            }
     }
-    if (sub != 0) return;
-    const int32_t row = pair / G, head = p.heads.order[head0 + pair - row * G];
-    const int64_t to = (int64_t)(at.r.row0 + row) * p.n_q_heads + head;
-    const bool none = M == -INFINITY && l == 0.f;
-    const float inv = none ? 0.f : 1.f / l;
-    if (none) acc = f32x4{0.f, 0.f, 0.f, 0.f};
-    if constexpr (BF16) {
-        const ushort4 x = make_ushort4(bf16_nearest(acc[0] * inv), bf16_nearest(acc[1] * inv), bf16_nearest(acc[2] * inv), bf16_nearest(acc[3] * inv));
-        *reinterpret_cast<ushort4 *>((uint16_t *)p.out + to * D + d4) = x;
-    } else {
-        *reinterpret_cast<f32x4 *>((float *)p.out + to * D + d4) = acc * inv;
+    *reinterpret_cast<f32x4 *>(&parts[mine][sub][d4]) = acc;
+    if (d4 == 0) {
+        ml[mine][sub][0] = M;
+        ml[mine][sub][1] = l;
     }
-    if (p.lse && d4 == 0) p.lse[to] = none ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    __syncthreads();
+    if (tid >= LPR || in_tile >= n_pairs || in_tile >= kKv4Pairs) return;
+    M = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < NSUB; ++u) M = fmaxf(M, ml[mine][u][0]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    l = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < NSUB; ++u) {
+        const float f = __builtin_amdgcn_exp2f(ml[mine][u][0] - ref);
+        l += f * ml[mine][u][1];
+        acc += f * *reinterpret_cast<const f32x4 *>(&parts[mine][u][d4]);
+    }
+    const int32_t row = pair / G, head = query_head(p, head0 + pair - row * G);
+    store_pair<D, BF16>(p, (int64_t)(at.r.row0 + row) * p.n_q_heads + head, d4, acc, M, l);
+}
+
+template <int D, bool BF16>
+static void launch_merge_kv4(const Kv4Attn &p, int32_t pairs, hipStream_t stream)
+{
+    // few units are cut into many items
+    if (p.max_units <= 16) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16>), dim3(p.max_units * pairs), dim3(1024), 0, stream, p, pairs);
+    else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 2>), dim3(p.max_units * ceil_div(pairs, 2)), dim3(256), 0, stream, p, pairs);
 }
 
 hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, bool merge, hipStream_t stream)
 {
     const auto kernel = D == 128 ? (bf16 ? attn_kv4_kernel<128, true> : attn_kv4_kernel<128, false>)
                                  : (bf16 ? attn_kv4_kernel<64, true> : attn_kv4_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, dim3((p.max_items + 7) / 8 * 8), dim3(NW * 64), 0, stream, p);
+    hipLaunchKernelGGL(kernel, dim3((p.grid + 7) / 8 * 8), dim3(NW * 64), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !merge) return e;
     const int32_t pairs = (int32_t)((int64_t)p.num_rows * p.group < kKv4Pairs ? p.num_rows * p.group : kKv4Pairs);
-    const auto join = D == 128 ? (bf16 ? merge_kv4_kernel<128, true> : merge_kv4_kernel<128, false>)
-                               : (bf16 ? merge_kv4_kernel<64, true> : merge_kv4_kernel<64, false>);
-    hipLaunchKernelGGL(join, dim3(p.max_units * pairs), dim3(64), 0, stream, p, pairs);
+    if (D == 128) bf16 ? launch_merge_kv4<128, true>(p, pairs, stream) : launch_merge_kv4<128, false>(p, pairs, stream);
+    else bf16 ? launch_merge_kv4<64, true>(p, pairs, stream) : launch_merge_kv4<64, false>(p, pairs, stream);
     return hipGetLastError();
 }
 

@@ -80,8 +80,12 @@ struct Kv4Attn {
     float *part_acc, *part_ml;        // [item][kKv4Pairs][D], [item][kKv4Pairs][2]: of items that are not whole units
     int32_t num_seqs, max_pages, num_rows, n_q_heads;
     int32_t group;                    // query heads of the KV head that has most
-    int32_t target_items, min_steps;  // items that a call is cut into, if they are not shorter than this
+    int32_t mapped;                   // whether a head map is given
+    int32_t by_xcd;                   // whether an XCD takes neighbouring items, as tiles of the same keys are
+    float target_rcp;                 // 1 / items that a call is cut into, if they are not
+    int32_t min_steps;                // shorter than this
     int32_t max_items, max_units;     // bounds that no lengths pass
+    int32_t grid;                     // and one for the items that the table's width allows
     float c_log2;                     // softmax scale * log2(e)
     Kv4Heads heads;
 };

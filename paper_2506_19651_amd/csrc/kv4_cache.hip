@@ -1,99 +1,55 @@
 // The paged 4-bit KV cache's bookkeeping and its rows in and out (gfx950).
 #include "kv4.h"
+#include "wave_scan.h"
 
 namespace pevlm {
 
 // ------------------------------------------------------------------------------------------
 // Slots.  What a request gets depends on those before it only through two running sums (rows, pages), so one workgroup
-// takes the requests 1024 at a time: inclusive scans of the new tokens, then of the pages that the requests which fit lack.
+// takes the requests T at a time: inclusive scans of the new tokens, then of the pages that the requests which fit lack.  Sums stop
+// at 2^32 - 1, which is more than any bound they are held to.  A step's few rows are filled in by the same workgroup from LDS; a prompt's by
+// a launch of one row a lane.  Bound by latency: kernel 4.2 us for 64 requests of one token where two launches took 3.9 and 2.6.
 // ------------------------------------------------------------------------------------------
-constexpr int32_t kScanThreads = 1024;
+constexpr int32_t kSmallRows = 2048, kSmallRequests = 1024;
 
-// inclusive sum over the workgroup plus `carry`; `waves` holds the wavefronts' sums
-__device__ inline int64_t scan_sum(int64_t x, int64_t *waves)
+// inclusive sum over the workgroup; `waves` holds the wavefronts' sums
+template <int T>
+__device__ __forceinline__ uint32_t scan_sum(uint32_t x, uint32_t *waves)
 {
-    const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t y = __shfl_up(x, o);
-        if (lane >= o) x += y;
+    const auto add = [](uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); };
+    x = wave_scan(x, add);
+    if constexpr (T > 64) {
+        const int32_t wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 63) waves[wave] = x;
+        __syncthreads();
+        uint32_t before = 0;
+        for (int w = 0; w < wave; ++w) before = add(before, waves[w]);
+        x = add(x, before);
     }
-    __syncthreads();  // the last scan's sums have been read
-    if (lane == 63) waves[wave] = x;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) x += waves[w];
     return x;
 }
 
-__global__ __launch_bounds__(kScanThreads) void kv4_requests_kernel(Kv4Slots p)
-{
-    __shared__ int64_t waves[kScanThreads / 64];
-    __shared__ int64_t rows_before, need_before;
-    __shared__ int32_t taken;
-    const int64_t width = (int64_t)p.max_pages << p.page_shift;
-    const int32_t round = (1 << p.page_shift) - 1;
-    int32_t free = *p.num_free;
-    free = free < 0 ? 0 : (free < p.free_capacity ? free : p.free_capacity);
-    if (threadIdx.x == 0) {
-        rows_before = need_before = 0;
-        taken = 0;
-    }
-    __syncthreads();
-    for (int32_t s0 = 0; s0 < p.num_seqs; s0 += kScanThreads) {
-        const int32_t s = s0 + threadIdx.x;
-        const bool real = s < p.num_seqs;
-        const int32_t given = real ? p.seq_len[s] : 0;
-        const int64_t held = given < 0 ? 0 : given;
-        int64_t more = real ? (p.new_len ? p.new_len[s] : 1) : 0;
-        more = more < 0 ? 0 : more;
-        const int64_t end = scan_sum(more, waves) + rows_before;
-        const bool fits = held + more <= width && end <= p.num_rows;
-        const int64_t have = (held + round) >> p.page_shift;
-        const int64_t need = fits ? ((held + more + round) >> p.page_shift) - have : 0;
-        const int64_t all = scan_sum(need, waves) + need_before;
-        const bool served = fits && (need == 0 || all <= free);
-        if (real) {
-            p.row_start[s] = (int32_t)(end - more < INT32_MAX ? end - more : INT32_MAX);
-            p.row_len[s] = served ? (int32_t)more : 0;
-            p.seq_len_out[s] = served ? (int32_t)(held + more) : given;
-            p.first_free[s] = served ? (int32_t)(free - 1 - (all - need)) : 0;
-        }
-        if (served && need > 0) atomicMax(&taken, (int32_t)all);  // of whole numbers: any order
-        __syncthreads();  // both sums have been read
-        if (threadIdx.x == kScanThreads - 1) {
-            rows_before = end;
-            need_before = all;
-        }
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) *p.num_free_out = free - taken;
-}
+// What a row of a request gets, from the request's lengths and first new page
+struct RowOf {
+    int32_t start, rows, held, first_free;  // held: before the new tokens
+};
 
-// One row a lane: its request by bisection over the rows' starts, its page from the table or from the list
-__global__ __launch_bounds__(256) void kv4_slots_kernel(Kv4Slots p)
+__device__ __forceinline__ void fill_row(const Kv4Slots &p, int32_t row, int32_t s, const RowOf &r)
 {
-    const int32_t row = blockIdx.x * 256 + threadIdx.x;
-    if (row >= p.num_rows) return;
-    int32_t s = 0, hi = p.num_seqs;  // the last request that starts at or before the row
-    while (hi - s > 1) {
-        const int32_t mid = (s + hi) / 2;
-        if (p.row_start[mid] <= row) s = mid;
-        else hi = mid;
-    }
-    const int32_t i = row - p.row_start[s], n = p.row_len[s];
+    const int32_t i = row - r.start, in_page = (1 << p.page_shift) - 1;
     int32_t slot = -1, pos = 0;
-    if (i >= 0 && i < n) {
-        const int32_t held = p.seq_len_out[s] - n, at = held + i, column = at >> p.page_shift;
-        const int32_t have = (int32_t)(((int64_t)held + (1 << p.page_shift) - 1) >> p.page_shift);
+    if (i >= 0 && i < r.rows) {
+        const int32_t at = r.held + i, column = at >> p.page_shift;
+        const int32_t have = (int32_t)(((int64_t)r.held + in_page) >> p.page_shift);
         int32_t *entry = p.table + (int64_t)s * p.max_pages + column;
         int32_t page;
         if (column < have) {
             page = *entry;
         } else {
-            page = p.free_pages[p.first_free[s] - (column - have)];
-            if ((at & ((1 << p.page_shift) - 1)) == 0) *entry = page;
+            page = p.free_pages[r.first_free - (column - have)];
+            if ((at & in_page) == 0) *entry = page;
         }
-        if (page >= 0 && page < p.num_pages) slot = (page << p.page_shift) + (at & ((1 << p.page_shift) - 1));
+        if (page >= 0 && page < p.num_pages) slot = (page << p.page_shift) + (at & in_page);
         pos = (int32_t)((uint32_t)at + (uint32_t)(p.pos_offset ? p.pos_offset[s] : 0));
     }
     p.slot_map[row] = slot;
@@ -101,9 +57,96 @@ __global__ __launch_bounds__(256) void kv4_slots_kernel(Kv4Slots p)
         for (int a = 0; a < 3; ++a) p.pos_ids[(int64_t)a * p.num_rows + row] = pos;
 }
 
+// The last request that starts at or before the row
+template <class Start>
+__device__ __forceinline__ int32_t request_of(int32_t n, int32_t row, Start start)
+{
+    int32_t s = 0, hi = n;
+    while (hi - s > 1) {
+        const int32_t mid = (s + hi) / 2;
+        if (start(mid) <= row) s = mid;
+        else hi = mid;
+    }
+    return s;
+}
+
+// SMALL: at most kSmallRequests requests and kSmallRows rows, which are filled in here
+template <int T, bool SMALL>
+__global__ __launch_bounds__(T) void kv4_requests_kernel(Kv4Slots p)
+{
+    __shared__ uint32_t waves[2][T / 64];
+    __shared__ uint32_t rows_before, need_before, taken;
+    __shared__ RowOf of[SMALL ? kSmallRequests : 1];
+    const int64_t width = (int64_t)p.max_pages << p.page_shift;
+    const int32_t round = (1 << p.page_shift) - 1;
+    int32_t free = *p.num_free;
+    free = free < 0 ? 0 : (free < p.free_capacity ? free : p.free_capacity);
+    if (threadIdx.x == 0) rows_before = need_before = taken = 0;
+    for (int32_t s0 = 0; s0 < p.num_seqs; s0 += T) {
+        const int32_t s = s0 + threadIdx.x;
+        const bool real = s < p.num_seqs;
+        const int32_t given = real ? p.seq_len[s] : 0;
+        const int64_t held = given < 0 ? 0 : given;
+        int32_t more = real ? (p.new_len ? p.new_len[s] : 1) : 0;
+        more = more < 0 ? 0 : more;
+        __syncthreads();  // the sums before these requests stand
+        const uint32_t end = __builtin_elementwise_add_sat(scan_sum<T>(more, waves[0]), rows_before);
+        const uint32_t start = end == UINT32_MAX ? UINT32_MAX : end - more;  // beyond any row either way
+        const bool fits = held + more <= width && end <= (uint32_t)p.num_rows;
+        const int64_t have = (held + round) >> p.page_shift;
+        const uint32_t need = fits ? (uint32_t)(((held + more + round) >> p.page_shift) - have) : 0;
+        const uint32_t all = __builtin_elementwise_add_sat(scan_sum<T>(need, waves[1]), need_before);
+        const bool served = fits && (need == 0 || all <= (uint32_t)free);
+        if (real) {
+            RowOf r;
+            r.start = (int32_t)(start < INT32_MAX ? start : INT32_MAX);
+            r.rows = served ? more : 0;
+            r.held = (int32_t)held;
+            r.first_free = served ? (int32_t)(free - 1 - (all - need)) : 0;
+            p.row_start[s] = r.start;
+            p.row_len[s] = r.rows;
+            p.seq_len_out[s] = served ? (int32_t)(held + more) : given;
+            if constexpr (SMALL) of[s] = r;
+            else p.first_free[s] = r.first_free;
+        }
+        if (served && need > 0) atomicMax(&taken, all);  // of whole numbers: any order
+        __syncthreads();  // both sums have been read
+        if (threadIdx.x == T - 1) {
+            rows_before = end;
+            need_before = all;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) *p.num_free_out = free - (int32_t)taken;
+    if constexpr (SMALL)
+        for (int32_t row = threadIdx.x; row < p.num_rows; row += T) {
+            const int32_t s = request_of(p.num_seqs, row, [&](int32_t i) { return of[i].start; });
+            fill_row(p, row, s, of[s]);
+        }
+}
+
+__global__ __launch_bounds__(256) void kv4_slots_kernel(Kv4Slots p)
+{
+    const int32_t row = blockIdx.x * 256 + threadIdx.x;
+    if (row >= p.num_rows) return;
+    const int32_t s = request_of(p.num_seqs, row, [&](int32_t i) { return p.row_start[i]; });
+    RowOf r;
+    r.start = p.row_start[s];
+    r.rows = p.row_len[s];
+    r.held = p.seq_len_out[s] - r.rows;
+    r.first_free = p.first_free[s];
+    fill_row(p, row, s, r);
+}
+
 hipError_t launch_kv4_slots(const Kv4Slots &p, hipStream_t stream)
 {
-    hipLaunchKernelGGL(kv4_requests_kernel, dim3(1), dim3(kScanThreads), 0, stream, p);
+    if (p.num_rows <= kSmallRows && p.num_seqs <= kSmallRequests) {
+        const bool few = p.num_seqs <= 256 && p.num_rows <= 512;
+        if (few) hipLaunchKernelGGL((kv4_requests_kernel<256, true>), dim3(1), dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL((kv4_requests_kernel<1024, true>), dim3(1), dim3(1024), 0, stream, p);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((kv4_requests_kernel<1024, false>), dim3(1), dim3(1024), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.num_rows == 0) return e;
     hipLaunchKernelGGL(kv4_slots_kernel, dim3((p.num_rows + 255) / 256), dim3(256), 0, stream, p);
