@@ -88,6 +88,7 @@ static void size_attn(const pevlm_heads *h, int32_t num_seqs, int32_t num_rows, 
     HeadTable tab;
     check_heads(h, &tab);
     p->group = group_heads(tab, h, &p->heads);
+    p->tile_pairs = (int32_t)std::min<int64_t>(kKv4Pairs, (int64_t)num_rows * p->group);
     const int64_t asking = std::min(num_seqs, num_rows);
     const int64_t units = h->n_kv_heads * (asking + (int64_t)num_rows * p->group / kKv4Pairs);
     const int32_t target = 6 * compute_units();
@@ -99,8 +100,8 @@ static void size_attn(const pevlm_heads *h, int32_t num_seqs, int32_t num_rows, 
     p->max_items = (int32_t)std::min<int64_t>(units + target + 8, INT32_MAX);
 }
 
-static size_t ml_bytes(const Kv4Attn &p) { return align256((size_t)p.max_items * kKv4Pairs * 2 * sizeof(float)); }
-static size_t attn_bytes(const Kv4Attn &p, int32_t D) { return ml_bytes(p) + align256((size_t)p.max_items * kKv4Pairs * D * sizeof(float)); }
+static size_t ml_bytes(const Kv4Attn &p) { return align256((size_t)p.max_items * p.tile_pairs * 2 * sizeof(float)); }
+static size_t attn_bytes(const Kv4Attn &p, int32_t D) { return ml_bytes(p) + align256((size_t)p.max_items * p.tile_pairs * D * sizeof(float)); }
 
 }  // namespace pevlm
 

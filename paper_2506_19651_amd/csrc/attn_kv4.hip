@@ -19,7 +19,7 @@ namespace {
 
 constexpr int NW = 4;  // wavefronts of a workgroup
 constexpr int AHEAD = 1;  // steps whose loads are under way before the one at hand
-constexpr int32_t kMany = 0x3fffffff;
+constexpr int32_t kMany = 0x3fffffff;  // two of them fit 31 bits
 
 // What a request's rows see: records (16 tokens) [0, n_sink) and [near, near + n_near), which do not overlap
 struct Span {
@@ -34,23 +34,24 @@ struct Request {
 __device__ __forceinline__ Request read_request(const Kv4Attn &p, int32_t s)
 {
     Request r;
-    const int64_t width = (int64_t)p.max_pages << p.pool.page_shift;
+    const int32_t width = p.max_pages << p.pool.page_shift;  // below 2^31
     r.row0 = p.row_start[s];
     r.rows = p.row_len[s];
     const int32_t len = p.seq_len[s];
-    r.held = len < 0 ? 0 : (len < width ? len : (int32_t)width);
     r.window = p.window ? p.window[s] : -1;
-    r.sink = p.sink_len && r.window >= 0 ? p.sink_len[s] : 0;
+    r.sink = p.window && p.sink_len ? p.sink_len[s] : 0;
+    r.held = len < 0 ? 0 : (len < width ? len : width);
+    if (r.window < 0) r.sink = 0;
     r.sink = r.sink < 0 ? 0 : (r.sink < r.held ? r.sink : r.held);
-    if (r.row0 < 0 || r.rows < 0 || (int64_t)r.row0 + r.rows > p.num_rows) r.rows = 0;
+    if (r.row0 < 0 || r.rows < 0 || r.rows > p.num_rows - r.row0) r.rows = 0;
     return r;
 }
 
-// first token inside the window of the token at position `pos`
+// First token inside the window of the token at position `pos`.  (Where the difference wraps, pos is negative and nothing is seen.)
 __device__ __forceinline__ int32_t near_of(const Request &r, int32_t pos)
 {
-    const int64_t n = (int64_t)pos - r.window + 1;
-    return r.window < 0 || n < 0 ? 0 : (int32_t)(n < r.held ? n : r.held);
+    const int32_t n = (int32_t)((uint32_t)pos - (uint32_t)r.window + 1u);
+    return r.window < 0 || n < 0 ? 0 : (n < r.held ? n : r.held);
 }
 
 __device__ __forceinline__ Span span_of(const Request &r)
@@ -71,6 +72,21 @@ __device__ __forceinline__ int32_t lane_value(int32_t x, int32_t lane) { return 
 // a value that is the same in every lane, where the compiler is to know it
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// x / d and the rest of it, x >= 0, d > 0.  Up to 2^20 in fp32: (x + 1/2) / d is at least 1 / (2 d) away from a whole number, and two
+// roundings move it by less.  (A whole-number division is some 40 instructions in a row, and a workgroup makes several before its first load.)
+__device__ __forceinline__ int32_t divide(int32_t x, int32_t d, int32_t &rest)
+{
+    const int32_t n = x < (1 << 20) ? (int32_t)(((float)x + 0.5f) * __builtin_amdgcn_rcpf((float)d)) : x / d;
+    rest = x - n * d;
+    return n;
+}
+__device__ __forceinline__ int32_t divide(int32_t x, int32_t d)
+{
+    int32_t rest;
+    return divide(x, d, rest);
+}
+__device__ __forceinline__ int32_t divide_up(int32_t x, int32_t d) { return divide(x + d - 1, d); }  // x + d below 2^31
+
 // Where the idx-th item (or unit) of a call lies.  Every wavefront finds its own by itself: lane by lane over 64 requests at a
 // time, once for the whole work, which sets the items' length, and once for the place.
 struct Place {
@@ -89,17 +105,17 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
         if (s < p.num_seqs) {
             r = read_request(p, s);
             if (r.rows > 0) {
-                tiles = r.rows * p.group <= kKv4Pairs ? 1 : (int32_t)(((int64_t)r.rows * p.group + kKv4Pairs - 1) / kKv4Pairs);
+                tiles = (r.rows * p.group + kKv4Pairs - 1) / kKv4Pairs;  // below 2^31: the host has looked at num_rows * group
                 steps = steps_of(span_of(r));
             }
         }
     };
     // Counts stop at kMany: with row ranges that overlap they can pass any bound, and no item or unit lies there
     const auto count = [&](int32_t n) {
-        const int64_t x = (int64_t)n * tiles * p.pool.n_kv_heads;
-        return (int32_t)(x < kMany ? x : kMany);
+        const float x = (float)n * (float)tiles * (float)p.pool.n_kv_heads;
+        return x < (float)kMany ? n * tiles * p.pool.n_kv_heads : kMany;
     };
-    const auto sum = [](int32_t a, int32_t b) { return a + b < kMany ? a + b : kMany; };
+    const auto sum = [](int32_t a, int32_t b) { return min(a + b, kMany); };
     const auto total = [](auto x) { return __builtin_bit_cast(decltype(x), lane_value(__builtin_bit_cast(int32_t, x), 63)); };
     float work = 0.f;  // what it rounds off moves the items' length by less than one part in 2^18, and max_items has room for that
     for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
@@ -108,7 +124,7 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
     }
     const float length = work * (float)p.pool.n_kv_heads * p.target_rcp;  // steps of an item
     const int32_t per = length < (float)p.min_steps ? p.min_steps : (length < 1e9f ? (int32_t)length + 1 : 1000000000);
-    const auto splits_of = [&] { return steps > per ? ceil_div(steps, per) : 1; };  // rows that see nothing are an item, too
+    const auto splits_of = [&] { return steps > per ? divide_up(steps, per) : 1; };  // rows that see nothing are an item, too
 
     Place at;
     at.s = -1;
@@ -148,18 +164,6 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
         at.first_item = sum(at.first_item, total(item_end));
     }
     return at;
-}
-
-// x / d and the rest of it
-__device__ __forceinline__ int32_t divide(int32_t x, int32_t d, int32_t &rest)
-{
-    if (d == 1) {
-        rest = 0;
-        return x;
-    }
-    const int32_t n = x / d;
-    rest = x - n * d;
-    return n;
 }
 
 // A KV head's query heads: as a map sorts them, or equal groups in order
@@ -228,7 +232,7 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
     const int32_t n_pairs = n_pairs_all - pair0 < kKv4Pairs ? n_pairs_all - pair0 : kKv4Pairs;
     if (n_pairs <= 0) return;
     const Span span = span_of(r);
-    const int32_t steps = steps_of(span), per = at.splits == 1 ? steps : ceil_div(steps, at.splits);
+    const int32_t steps = steps_of(span), per = divide_up(steps, at.splits);
     const int32_t step0 = split * per, step1 = step0 + per < steps ? step0 + per : steps;
 
     const int32_t tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, kg = lane >> 4;
@@ -237,10 +241,11 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
 
     // this lane's pair (column of S^T)
     const int32_t pair = pair0 + (l16 < n_pairs ? l16 : n_pairs - 1);
-    const int32_t row = pair / G, head = query_head(p, head0 + pair - row * G);
+    int32_t in_row;
+    const int32_t row = divide(pair, G, in_row), head = query_head(p, head0 + in_row);
     const int32_t pos = r.held - r.rows + row, near = near_of(r, pos);
     // the tile's first and last rows: positions and windows rise with the row
-    const int32_t pos_lo = r.held - r.rows + pair0 / G, pos_hi = r.held - r.rows + (pair0 + n_pairs - 1) / G;
+    const int32_t pos_lo = r.held - r.rows + divide(pair0, G), pos_hi = r.held - r.rows + divide(pair0 + n_pairs - 1, G);
     const int32_t near_lo = near_of(r, pos_lo), near_hi = near_of(r, pos_hi);
 
     // ---- queries: the lane's pair, elements kg * (D / 4) + 8 m .. + 8 of k-step m
@@ -269,23 +274,25 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
     }
 
     // ---- the wavefront's records, 64 steps at a time: lane i holds those of step i of them
-    int64_t rec_off[2];
+    uint64_t rec_off[2];
     int32_t rec_tok[2];  // first token; -1: a record that is not there
+    const int32_t *const table = p.table + (int64_t)at.s * p.max_pages;
+    const int32_t rec_shift = p.pool.page_shift - 4;
+    const uint32_t head_bytes = (uint32_t)C::BYTES << rec_shift, page_bytes = head_bytes * p.pool.n_kv_heads, head_off = head_bytes * g;
     const auto read_records = [&](int32_t first) {  // first: the wavefront's steps before these
         const int32_t st = step0 + wave + (first + lane) * NW;
+        int32_t rec[2], page[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int32_t v = st * 2 + e;
-            rec_tok[e] = -1;
-            rec_off[e] = 0;
-            if (st < step1 && v < span.records) {
-                const int32_t rec = v < span.n_sink ? v : v - span.n_sink + span.near;
-                const int32_t page = p.table[(int64_t)at.s * p.max_pages + (rec >> (p.pool.page_shift - 4))];
-                if (page >= 0 && page < p.pool.num_pages) {
-                    rec_tok[e] = rec * kKv4Record;
-                    rec_off[e] = kv4_record<D>(p.pool, page, g, rec & ((1 << (p.pool.page_shift - 4)) - 1));
-                }
-            }
+            rec[e] = st < step1 && v < span.records ? (v < span.n_sink ? v : v - span.n_sink + span.near) : -1;
+            page[e] = table[(rec[e] < 0 ? 0 : rec[e]) >> rec_shift];
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const bool there = rec[e] >= 0 && page[e] >= 0 && page[e] < p.pool.num_pages;
+            rec_tok[e] = there ? rec[e] * kKv4Record : -1;
+            rec_off[e] = there ? (uint64_t)(uint32_t)page[e] * page_bytes + head_off + (uint32_t)(rec[e] & ((1 << rec_shift) - 1)) * C::BYTES : 0;
         }
     };
 
@@ -300,7 +307,7 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
     const auto fetch = [&](Step &st, int32_t i) {  // the i-th of those steps
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int64_t off = (int64_t)((uint64_t)(uint32_t)lane_value((int32_t)(rec_off[e] >> 32), i) << 32 | (uint32_t)lane_value((int32_t)rec_off[e], i));
+            const uint64_t off = (uint64_t)(uint32_t)lane_value((int32_t)(rec_off[e] >> 32), i) << 32 | (uint32_t)lane_value((int32_t)rec_off[e], i);
             st.tok[e] = lane_value(rec_tok[e], i);
             const uint8_t *base = p.pool.base + off;
             if constexpr (D == 128) {
@@ -473,14 +480,16 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
             acc += f * *reinterpret_cast<const f32x4 *>(all_o + (w * kKv4Pairs + pr) * D + d4);
         }
         if (at.splits > 1) {
-            const int64_t slot = (int64_t)item * kKv4Pairs + pr;
+            const int64_t slot = (int64_t)item * p.tile_pairs + pr;
             *reinterpret_cast<f32x4 *>(p.part_acc + slot * D + d4) = acc;
             if (d4 == 0) {
                 p.part_ml[slot * 2] = M;
                 p.part_ml[slot * 2 + 1] = l;
             }
         } else {
-            const int32_t pp = pair0 + pr, rr = pp / G, hh = query_head(p, head0 + pp - rr * G);
+            int32_t hh;
+            const int32_t rr = divide(pair0 + pr, G, hh);
+            hh = query_head(p, head0 + hh);
             store_pair<D, BF16>(p, (int64_t)(r.row0 + rr) * p.n_q_heads + hh, d4, acc, M, l);
         }
     }
@@ -493,12 +502,12 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
 constexpr int kTurn = 6;
 
 template <int D, bool BF16, int WAVES>
-__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void merge_kv4_kernel(Kv4Attn p, int32_t pairs_of_unit)
+__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void merge_kv4_kernel(Kv4Attn p)
 {
     constexpr int LPR = D / 4, NSUB = WAVES * 64 / LPR, PAIRS = WAVES == 16 ? 1 : 4 / WAVES;
-    __shared__ float parts[PAIRS][NSUB][D], ml[PAIRS][NSUB][2];
+    __shared__ float parts[PAIRS][WAVES][D], ml[PAIRS][WAVES][2];
     int32_t pr;
-    const int32_t unit = divide(blockIdx.x, ceil_div(pairs_of_unit, PAIRS), pr);
+    const int32_t unit = divide(blockIdx.x, (p.tile_pairs + PAIRS - 1) / PAIRS, pr);
     const Place at = find_place<true>(p, unit);
     if (at.s < 0 || at.splits < 2) return;
     int32_t tile;
@@ -510,7 +519,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void merge_kv4_kernel(Kv4
     if (item0 + (int64_t)(at.splits - 1) * at.tiles >= p.max_items) return;
     const int32_t mine = __builtin_amdgcn_readfirstlane(threadIdx.x / (WAVES * 64)), tid = threadIdx.x % (WAVES * 64);
     const int32_t in_tile = pr * PAIRS + mine, pair = tile * kKv4Pairs + in_tile;
-    const int64_t slot0 = item0 * kKv4Pairs + in_tile, stride = (int64_t)at.tiles * kKv4Pairs;
+    const int64_t slot0 = item0 * p.tile_pairs + (in_tile < p.tile_pairs ? in_tile : p.tile_pairs - 1), stride = (int64_t)at.tiles * p.tile_pairs;
     const int32_t sub = tid / LPR, d4 = tid % LPR * 4;
     float M = -INFINITY, l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -539,47 +548,68 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void merge_kv4_kernel(Kv4
                 acc += f * a[u];
             }
     }
-    *reinterpret_cast<f32x4 *>(&parts[mine][sub][d4]) = acc;
-    if (d4 == 0) {
-        ml[mine][sub][0] = M;
-        ml[mine][sub][1] = l;
+    // the groups of a wavefront in registers, the wavefronts through LDS
+    const auto join = [&](float M2, float l2, f32x4 acc2) {
+        const float top = fmaxf(M, M2), ref = top == -INFINITY ? 0.f : top;
+        const float f = __builtin_amdgcn_exp2f(M - ref), f2 = __builtin_amdgcn_exp2f(M2 - ref);
+        l = f * l + f2 * l2;
+        acc = f * acc + f2 * acc2;
+        M = top;
+    };
+#pragma unroll
+    for (int o = LPR; o < 64; o <<= 1) {
+        const f32x4 other = {__shfl_xor(acc[0], o), __shfl_xor(acc[1], o), __shfl_xor(acc[2], o), __shfl_xor(acc[3], o)};
+        join(__shfl_xor(M, o), __shfl_xor(l, o), other);
+    }
+    const int32_t wave = tid >> 6;
+    if ((tid & 63) < LPR) {
+        *reinterpret_cast<f32x4 *>(&parts[mine][wave][d4]) = acc;
+        if (d4 == 0) {
+            ml[mine][wave][0] = M;
+            ml[mine][wave][1] = l;
+        }
     }
     __syncthreads();
     if (tid >= LPR || in_tile >= n_pairs || in_tile >= kKv4Pairs) return;
+    float Ms[WAVES], ls[WAVES];
+    f32x4 as[WAVES];
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        Ms[w] = ml[mine][w][0];
+        ls[w] = ml[mine][w][1];
+        as[w] = *reinterpret_cast<const f32x4 *>(&parts[mine][w][d4]);
+    }
     M = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < NSUB; ++u) M = fmaxf(M, ml[mine][u][0]);
+    for (int w = 0; w < WAVES; ++w) M = fmaxf(M, Ms[w]);
     const float ref = M == -INFINITY ? 0.f : M;
     l = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < NSUB; ++u) {
-        const float f = __builtin_amdgcn_exp2f(ml[mine][u][0] - ref);
-        l += f * ml[mine][u][1];
-        acc += f * *reinterpret_cast<const f32x4 *>(&parts[mine][u][d4]);
+    for (int w = 0; w < WAVES; ++w) {
+        const float f = __builtin_amdgcn_exp2f(Ms[w] - ref);
+        l += f * ls[w];
+        acc += f * as[w];
     }
-    const int32_t row = pair / G, head = query_head(p, head0 + pair - row * G);
+    int32_t in_row;
+    const int32_t row = divide(pair, G, in_row), head = query_head(p, head0 + in_row);
     store_pair<D, BF16>(p, (int64_t)(at.r.row0 + row) * p.n_q_heads + head, d4, acc, M, l);
 }
 
 template <int D, bool BF16>
-static void launch_merge_kv4(const Kv4Attn &p, int32_t pairs, hipStream_t stream)
+static void launch(const Kv4Attn &p, bool merge, hipStream_t stream)
 {
+    hipLaunchKernelGGL((attn_kv4_kernel<D, BF16>), dim3((p.grid + 7) / 8 * 8), dim3(NW * 64), 0, stream, p);
+    if (!merge) return;
     // few units are cut into many items
-    if (p.max_units <= 16) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16>), dim3(p.max_units * pairs), dim3(1024), 0, stream, p, pairs);
-    else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 2>), dim3(p.max_units * ceil_div(pairs, 2)), dim3(256), 0, stream, p, pairs);
+    if (p.max_units <= 16) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16>), dim3(p.max_units * p.tile_pairs), dim3(1024), 0, stream, p);
+    else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 2>), dim3(p.max_units * ceil_div(p.tile_pairs, 2)), dim3(256), 0, stream, p);
 }
 
 hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, bool merge, hipStream_t stream)
 {
-    const auto kernel = D == 128 ? (bf16 ? attn_kv4_kernel<128, true> : attn_kv4_kernel<128, false>)
-                                 : (bf16 ? attn_kv4_kernel<64, true> : attn_kv4_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, dim3((p.grid + 7) / 8 * 8), dim3(NW * 64), 0, stream, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !merge) return e;
-    const int32_t pairs = (int32_t)((int64_t)p.num_rows * p.group < kKv4Pairs ? p.num_rows * p.group : kKv4Pairs);
-    if (D == 128) bf16 ? launch_merge_kv4<128, true>(p, pairs, stream) : launch_merge_kv4<128, false>(p, pairs, stream);
-    else bf16 ? launch_merge_kv4<64, true>(p, pairs, stream) : launch_merge_kv4<64, false>(p, pairs, stream);
+    if (D == 128) bf16 ? launch<128, true>(p, merge, stream) : launch<128, false>(p, merge, stream);
+    else bf16 ? launch<64, true>(p, merge, stream) : launch<64, false>(p, merge, stream);
     return hipGetLastError();
 }
 

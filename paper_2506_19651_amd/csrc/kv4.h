@@ -77,8 +77,9 @@ struct Kv4Attn {
     float *lse;
     Kv4Pool pool;
     const int32_t *table, *row_start, *row_len, *seq_len, *sink_len, *window;
-    float *part_acc, *part_ml;        // [item][kKv4Pairs][D], [item][kKv4Pairs][2]: of items that are not whole units
+    float *part_acc, *part_ml;        // [item][tile_pairs][D], [item][tile_pairs][2]: of items that are not whole units
     int32_t num_seqs, max_pages, num_rows, n_q_heads;
+    int32_t tile_pairs;               // pairs that a tile can have: kKv4Pairs, or all that the rows make
     int32_t group;                    // query heads of the KV head that has most
     int32_t mapped;                   // whether a head map is given
     int32_t by_xcd;                   // whether an XCD takes neighbouring items, as tiles of the same keys are

@@ -154,8 +154,41 @@ hipError_t launch_kv4_slots(const Kv4Slots &p, hipStream_t stream)
 }
 
 // ------------------------------------------------------------------------------------------
-// Rows in: a lane encodes one block of 32 elements.
+// Rows in and out.  A wavefront takes kRowsAt rows of one KV head, K and V.  A lane has 8 neighbouring elements of a row (chunk
+// l % (D / 8)), so that the wavefront's loads cover whole rows; four lanes make a block and find its scale.  What lane c of the four
+// encodes of their four rows is one word of each row's 16 bytes: a transpose within the four gives every lane the 16 bytes of one row,
+// and a wavefront's store is a record's codes as they lie, if its rows are neighbours in the cache.  Out the same way back.  Bound by HBM.
 // ------------------------------------------------------------------------------------------
+template <int D>
+struct RowsCfg {
+    static constexpr int CH = D / 8;        // chunks of a row
+    static constexpr int PER_LOAD = 64 / CH; // rows that one load of 8 elements a lane covers
+    static constexpr int ROWS = 4 * PER_LOAD;
+};
+
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E;  // quad_perm of the neighbour, and of the one after the next
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t quad(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int32_t)x, CTRL, 0xf, 0xf, true);
+}
+
+// w[i] of lane c of four becomes w[c] of lane i
+__device__ __forceinline__ void transpose_quad(uint32_t (&w)[4], int32_t c)
+{
+    const auto swap = [&](uint32_t &a, uint32_t &b, bool upper, auto from) {
+        const uint32_t x = from(upper ? a : b);
+        (upper ? a : b) = x;
+    };
+    const auto one = [](uint32_t x) { return quad<kXor1>(x); };
+    const auto two = [](uint32_t x) { return quad<kXor2>(x); };
+    swap(w[0], w[1], c & 1, one);
+    swap(w[2], w[3], c & 1, one);
+    swap(w[0], w[2], c & 2, two);
+    swap(w[1], w[3], c & 2, two);
+}
+
 // Exponent of a block's scale from the bits of its largest magnitude a = 1.f * 2^(E - 127): the smallest e with a <= 6 * 2^e
 __device__ __forceinline__ int32_t kv4_exponent(uint32_t a)
 {
@@ -164,104 +197,186 @@ __device__ __forceinline__ int32_t kv4_exponent(uint32_t a)
     return e < kKv4MinExp ? kKv4MinExp : (e > kKv4MaxExp ? kKv4MaxExp : e);
 }
 
-// Code of y, to nearest, ties to the even code
-__device__ __forceinline__ uint32_t kv4_code(float y)
+// Where a slot lies in the pool; < 0: nowhere
+template <int D>
+__device__ __forceinline__ int64_t slot_record(const Kv4Pool &p, int32_t slot, int32_t head, int32_t &t)
 {
-    const float m = fabsf(y);
-    const uint32_t c = (m > 0.25f) + (m >= 0.75f) + (m > 1.25f) + (m >= 1.75f) + (m > 2.5f) + (m >= 3.5f) + (m > 5.f);
-    return c | (__float_as_uint(y) >> 31) << 3;
+    t = slot & (kKv4Record - 1);
+    const int32_t page = slot >> p.page_shift;
+    if (slot < 0 || page >= p.num_pages) return -1;
+    return kv4_record<D>(p, page, head, (slot & ((1 << p.page_shift) - 1)) / kKv4Record);
+}
+
+// 8 elements of a row (BF16: one word has two, else one)
+template <bool BF16>
+struct Chunk {
+    uint32_t w[BF16 ? 4 : 8];
+};
+template <bool BF16>
+__device__ __forceinline__ Chunk<BF16> load_chunk(const void *rows, int64_t at)
+{
+    Chunk<BF16> x;
+    const uint4 *src = reinterpret_cast<const uint4 *>((const char *)rows + at * (BF16 ? 2 : 4));
+    const uint4 a = src[0];
+    x.w[0] = a.x; x.w[1] = a.y; x.w[2] = a.z; x.w[3] = a.w;
+    if constexpr (!BF16) {
+        const uint4 b = src[1];
+        x.w[4] = b.x; x.w[5] = b.y; x.w[6] = b.z; x.w[7] = b.w;
+    }
+    return x;
+}
+
+// The lane's word of codes and its block's scale byte
+template <bool BF16>
+__device__ __forceinline__ uint32_t encode_chunk(const Chunk<BF16> &x, uint32_t &scale_byte)
+{
+    uint32_t a = 0;
+    if constexpr (BF16) {
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t hi = x.w[i] & 0x7fff0000u, lo = x.w[i] << 16 & 0x7fff0000u;
+            a = max(a, max(hi, lo));
+        }
+    } else {
+        for (int i = 0; i < 8; ++i) a = max(a, x.w[i] & 0x7fffffffu);
+    }
+    a = max(a, quad<kXor1>(a));
+    a = max(a, quad<kXor2>(a));
+    const int32_t e = kv4_exponent(a);
+    const float scale = exp2_int(e);
+    uint32_t codes = 0;
+    if constexpr (BF16) {
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, x.w[0]), scale, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, x.w[1]), scale, 1);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, x.w[2]), scale, 2);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, x.w[3]), scale, 3);
+    } else {
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, __uint_as_float(x.w[0]), __uint_as_float(x.w[1]), scale, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, __uint_as_float(x.w[2]), __uint_as_float(x.w[3]), scale, 1);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, __uint_as_float(x.w[4]), __uint_as_float(x.w[5]), scale, 2);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, __uint_as_float(x.w[6]), __uint_as_float(x.w[7]), scale, 3);
+    }
+    const bool fine = a < 0x7f800000u;
+    scale_byte = fine ? e + kKv4Bias : kKv4NanScale;
+    return fine ? codes : 0;
+}
+
+// The lanes' places: chunk of the row, lane of its four, block; rows row0 + i * PER_LOAD of the group that the lane reads or writes
+// as chunks, the row c * PER_LOAD of them whose codes it has.
+template <int D>
+struct RowLane {
+    int32_t c, block, chunk, row;
+    __device__ __forceinline__ RowLane()
+    {
+        const int32_t lane = threadIdx.x & 63;
+        chunk = lane % RowsCfg<D>::CH;
+        row = lane / RowsCfg<D>::CH;
+        c = chunk & 3;
+        block = chunk >> 2;
+    }
+};
+
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void kv4_store_kernel(Kv4Rows p, int32_t groups)
+{
+    using R = RowsCfg<D>;
+    const int32_t id = blockIdx.x * 4 + (threadIdx.x >> 6), head = id % p.pool.n_kv_heads, group = id / p.pool.n_kv_heads;
+    if (group >= groups) return;
+    const RowLane<D> L;
+    const int32_t row0 = group * R::ROWS + L.row, mine = row0 + L.c * R::PER_LOAD;
+    const int32_t slot = mine < p.num_rows ? p.slot_map[mine] : -1;
+    Chunk<BF16> k[4], v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int32_t row = row0 + i * R::PER_LOAD, at = row < p.num_rows ? row : p.num_rows - 1;
+        const int64_t in_row = head * D + L.chunk * 8;
+        k[i] = load_chunk<BF16>(p.k, at * p.k_stride + in_row);
+        v[i] = load_chunk<BF16>(p.v, at * p.v_stride + in_row);
+    }
+    uint32_t kw[4], vw[4], scales = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t ks, vs;
+        kw[i] = encode_chunk<BF16>(k[i], ks);
+        vw[i] = encode_chunk<BF16>(v[i], vs);
+        if (L.c == i) scales = ks | vs << 8;
+    }
+    transpose_quad(kw, L.c);
+    transpose_quad(vw, L.c);
+    int32_t t;
+    const int64_t rec = slot_record<D>(p.pool, slot, head, t);
+    if (rec < 0) return;
+    uint8_t *base = p.pool.base + rec;
+    *reinterpret_cast<uint4 *>(base + (L.block * 16 + t) * 16) = make_uint4(kw[0], kw[1], kw[2], kw[3]);
+    *reinterpret_cast<uint4 *>(base + Kv4Cfg<D>::CODES + (L.block * 16 + t) * 16) = make_uint4(vw[0], vw[1], vw[2], vw[3]);
+    *reinterpret_cast<uint16_t *>(base + Kv4Cfg<D>::SCALES + (L.block * 16 + t) * 2) = (uint16_t)scales;
 }
 
 template <bool BF16>
-__device__ __forceinline__ float kv4_element(const void *row, int32_t i)
+__device__ __forceinline__ void store_chunk(void *rows, int64_t at, uint32_t codes, float scale)
 {
-    return BF16 ? __uint_as_float((uint32_t)((const uint16_t *)row)[i] << 16) : ((const float *)row)[i];
-}
-
-template <int D, bool BF16>
-__global__ __launch_bounds__(256) void kv4_store_kernel(Kv4Rows p)
-{
-    constexpr int NB = Kv4Cfg<D>::NB;
-    const int64_t per_row = (int64_t)p.pool.n_kv_heads * 2 * NB;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= p.num_rows * per_row) return;
-    const int32_t row = (int32_t)(id / per_row), unit = (int32_t)(id % per_row);
-    const int32_t b = unit % NB, which = unit / NB % 2, head = unit / (2 * NB);
-    const int32_t slot = p.slot_map[row];
-    if (slot < 0 || slot >> p.pool.page_shift >= p.pool.num_pages) return;
-    const size_t e = BF16 ? 2 : 4;
-    const void *src = (const char *)(which ? p.v : p.k) + ((int64_t)row * (which ? p.v_stride : p.k_stride) + head * D + b * 32) * e;
-    float x[32];
-    uint32_t amax = 0;
-    for (int i = 0; i < 32; ++i) {
-        x[i] = kv4_element<BF16>(src, i);
-        const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
-        amax = a > amax ? a : amax;
+    bf16x2 x[4];
+    kv4_decode8(codes, scale, x);  // exact in either type: a value has two significant bits
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = __builtin_bit_cast(uint32_t, x[j]);
+    uint4 *dst = reinterpret_cast<uint4 *>((char *)rows + at * (BF16 ? 2 : 4));
+    if constexpr (BF16) {
+        dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        dst[0] = make_uint4(w[0] << 16, w[0] & 0xffff0000u, w[1] << 16, w[1] & 0xffff0000u);
+        dst[1] = make_uint4(w[2] << 16, w[2] & 0xffff0000u, w[3] << 16, w[3] & 0xffff0000u);
     }
-    const bool fine = amax < 0x7f800000u;
-    const int32_t exp = kv4_exponent(amax);
-    const float f = exp2_int(-exp);
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (fine)
-        for (int i = 0; i < 32; ++i) w[i / 8] |= kv4_code(x[i] * f) << (i % 8 * 4);
-    const int32_t in_page = slot & ((1 << p.pool.page_shift) - 1), t = in_page % kKv4Record;
-    uint8_t *rec = p.pool.base + kv4_record<D>(p.pool, slot >> p.pool.page_shift, head, in_page / kKv4Record);
-    *reinterpret_cast<uint4 *>(rec + which * Kv4Cfg<D>::CODES + (b * 16 + t) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
-    rec[Kv4Cfg<D>::SCALES + (b * 16 + t) * 2 + which] = (uint8_t)(fine ? exp + kKv4Bias : kKv4NanScale);
 }
 
-// Rows out: a lane decodes one block
 template <int D, bool BF16>
-__global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows p)
+__global__ __launch_bounds__(256) void kv4_load_kernel(Kv4Rows p, int32_t groups)
 {
-    constexpr int NB = Kv4Cfg<D>::NB;
-    const int64_t per_row = (int64_t)p.pool.n_kv_heads * 2 * NB;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= p.num_rows * per_row) return;
-    const int32_t row = (int32_t)(id / per_row), unit = (int32_t)(id % per_row);
-    const int32_t b = unit % NB, which = unit / NB % 2, head = unit / (2 * NB);
-    const int32_t slot = p.slot_map[row];
-    if (slot < 0 || slot >> p.pool.page_shift >= p.pool.num_pages) return;
-    const int32_t in_page = slot & ((1 << p.pool.page_shift) - 1), t = in_page % kKv4Record;
-    const uint8_t *rec = p.pool.base + kv4_record<D>(p.pool, slot >> p.pool.page_shift, head, in_page / kKv4Record);
-    const uint4 c = *reinterpret_cast<const uint4 *>(rec + which * Kv4Cfg<D>::CODES + (b * 16 + t) * 16);
-    const float scale = kv4_scale(rec[Kv4Cfg<D>::SCALES + (b * 16 + t) * 2 + which]);
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    const int64_t to = (int64_t)row * (which ? p.v_stride : p.k_stride) + head * D + b * 32;
-    void *dst = which ? p.v : p.k;
+    using R = RowsCfg<D>;
+    const int32_t id = blockIdx.x * 4 + (threadIdx.x >> 6), head = id % p.pool.n_kv_heads, group = id / p.pool.n_kv_heads;
+    if (group >= groups) return;
+    const RowLane<D> L;
+    const int32_t row0 = group * R::ROWS + L.row, mine = row0 + L.c * R::PER_LOAD;
+    const int32_t slot = mine < p.num_rows ? p.slot_map[mine] : -1;
+    int32_t t;
+    const int64_t rec = slot_record<D>(p.pool, slot, head, t);
+    uint32_t kw[4] = {}, vw[4] = {}, scales = 0;
+    if (rec >= 0) {
+        const uint8_t *base = p.pool.base + rec;
+        const uint4 k = *reinterpret_cast<const uint4 *>(base + (L.block * 16 + t) * 16);
+        const uint4 v = *reinterpret_cast<const uint4 *>(base + Kv4Cfg<D>::CODES + (L.block * 16 + t) * 16);
+        scales = *reinterpret_cast<const uint16_t *>(base + Kv4Cfg<D>::SCALES + (L.block * 16 + t) * 2) | 1u << 16;  // and: there is such a row
+        kw[0] = k.x; kw[1] = k.y; kw[2] = k.z; kw[3] = k.w;
+        vw[0] = v.x; vw[1] = v.y; vw[2] = v.z; vw[3] = v.w;
+    }
+    transpose_quad(kw, L.c);
+    transpose_quad(vw, L.c);
+    const uint32_t of_row[4] = {quad<0x00>(scales), quad<0x55>(scales), quad<0xAA>(scales), quad<0xFF>(scales)};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        bf16x2 x[4];
-        kv4_decode8(w[i], scale, x);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t two = __builtin_bit_cast(uint32_t, x[j]);  // exact: a value has two significant bits
-            const int64_t at = to + i * 8 + j * 2;
-            if (BF16) *reinterpret_cast<uint32_t *>((uint16_t *)dst + at) = two;
-            else *reinterpret_cast<float2 *>((float *)dst + at) = make_float2(__uint_as_float(two << 16), __uint_as_float(two & 0xffff0000u));
-        }
+        if (!(of_row[i] >> 16)) continue;
+        const int64_t row = row0 + i * R::PER_LOAD, in_row = head * D + L.chunk * 8;
+        store_chunk<BF16>(p.k, row * p.k_stride + in_row, kw[i], kv4_scale(of_row[i] & 255u));
+        store_chunk<BF16>(p.v, row * p.v_stride + in_row, vw[i], kv4_scale(of_row[i] >> 8 & 255u));
     }
 }
 
-static dim3 blocks_grid(const Kv4Rows &p, int32_t D)
+template <int D, bool BF16>
+static hipError_t launch_rows(const Kv4Rows &p, bool in, hipStream_t stream)
 {
-    return dim3((uint32_t)(((int64_t)p.num_rows * p.pool.n_kv_heads * 2 * (D / 32) + 255) / 256));
-}
-
-hipError_t launch_kv4_store(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream)
-{
-    const auto kernel = D == 128 ? (bf16 ? kv4_store_kernel<128, true> : kv4_store_kernel<128, false>)
-                                 : (bf16 ? kv4_store_kernel<64, true> : kv4_store_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, blocks_grid(p, D), dim3(256), 0, stream, p);
+    const int32_t groups = ceil_div(p.num_rows, RowsCfg<D>::ROWS);
+    const dim3 grid((uint32_t)(((int64_t)groups * p.pool.n_kv_heads + 3) / 4));
+    if (in) hipLaunchKernelGGL((kv4_store_kernel<D, BF16>), grid, dim3(256), 0, stream, p, groups);
+    else hipLaunchKernelGGL((kv4_load_kernel<D, BF16>), grid, dim3(256), 0, stream, p, groups);
     return hipGetLastError();
 }
 
-hipError_t launch_kv4_load(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream)
+static hipError_t launch_rows(const Kv4Rows &p, int32_t D, bool bf16, bool in, hipStream_t stream)
 {
-    const auto kernel = D == 128 ? (bf16 ? kv4_load_kernel<128, true> : kv4_load_kernel<128, false>)
-                                 : (bf16 ? kv4_load_kernel<64, true> : kv4_load_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, blocks_grid(p, D), dim3(256), 0, stream, p);
-    return hipGetLastError();
+    if (D == 128) return bf16 ? launch_rows<128, true>(p, in, stream) : launch_rows<128, false>(p, in, stream);
+    return bf16 ? launch_rows<64, true>(p, in, stream) : launch_rows<64, false>(p, in, stream);
 }
+
+hipError_t launch_kv4_store(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream) { return launch_rows(p, D, bf16, true, stream); }
+hipError_t launch_kv4_load(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream) { return launch_rows(p, D, bf16, false, stream); }
 
 }  // namespace pevlm
