@@ -10,6 +10,9 @@ namespace pevlm {
 
 constexpr int32_t kMinPage = 16, kMaxPage = 4096;
 
+// Pairs of (row, query head) of a KV head and request, on average, above which the kernel of many rows is taken
+constexpr int64_t kManyPairs = 48;
+
 static bool page_size_ok(int32_t n) { return n >= kMinPage && n <= kMaxPage && (n & (n - 1)) == 0; }
 
 static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -82,22 +85,24 @@ static int32_t group_heads(const HeadTable &tab, const pevlm_heads *h, Kv4Heads 
     return most;
 }
 
-// What bounds a call's items, and how it is cut.  A request with r rows has ceil(r * group / kKv4Pairs) tiles of a KV head.
+// What bounds a call's items, and how it is cut.  A request with r rows has ceil(r * group / tile) tiles of a KV head.
 static void size_attn(const pevlm_heads *h, int32_t num_seqs, int32_t num_rows, Kv4Attn *p)
 {
     HeadTable tab;
     check_heads(h, &tab);
     p->group = group_heads(tab, h, &p->heads);
-    p->tile_pairs = (int32_t)std::min<int64_t>(kKv4Pairs, (int64_t)num_rows * p->group);
-    const int64_t asking = std::min(num_seqs, num_rows);
-    const int64_t units = h->n_kv_heads * (asking + (int64_t)num_rows * p->group / kKv4Pairs);
-    const int32_t target = 6 * compute_units();
-    p->target_rcp = 1.f / (float)target;
-    p->min_steps = 12;
     p->mapped = h->kv_head_of_q != nullptr;
-    p->by_xcd = p->group > kKv4Pairs || (int64_t)num_rows * p->group > (int64_t)kKv4Pairs * num_seqs;
+    const int64_t asking = std::max(1, std::min(num_seqs, num_rows)), pairs = (int64_t)num_rows * p->group;
+    const bool many = h->dtype == PEVLM_BF16 && pairs > kManyPairs * asking;
+    p->tile_shift = many ? kKv4RowsTileShift : kKv4TileShift;
+    p->step_shift = many ? kKv4RowsStepShift : kKv4StepShift;
+    p->tile_pairs = (int32_t)std::min<int64_t>(1 << p->tile_shift, pairs);
+    p->target = (many ? 2 : 6) * compute_units();
+    p->min_steps = many ? 8 : 12;
+    p->by_xcd = pairs > asking << p->tile_shift;
+    const int64_t units = h->n_kv_heads * (asking + (pairs >> p->tile_shift));
     p->max_units = (int32_t)std::min<int64_t>(units, INT32_MAX);
-    p->max_items = (int32_t)std::min<int64_t>(units + target + 8, INT32_MAX);
+    p->max_items = (int32_t)std::min<int64_t>(units + p->target + 8, INT32_MAX);
 }
 
 static size_t ml_bytes(const Kv4Attn &p) { return align256((size_t)p.max_items * p.tile_pairs * 2 * sizeof(float)); }
@@ -212,7 +217,7 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
     for (const int32_t *a : {row_start, row_len, seq_len, sink_len, window, (const int32_t *)lse})
         if (!aligned4(a)) return fail(PEVLM_ERR_INVALID_ARG, "arrays must be 4-byte aligned");
     size_attn(heads, cache->num_seqs, num_rows, &p);
-    if (p.max_items > 0x3fffffff || (int64_t)p.max_units * kKv4Pairs > INT32_MAX) return fail(PEVLM_ERR_UNSUPPORTED, "too many work items");
+    if (p.max_items > 0x3fffffff || ((int64_t)p.max_units << p.tile_shift) > INT32_MAX) return fail(PEVLM_ERR_UNSUPPORTED, "too many work items");
     const size_t need = attn_bytes(p, heads->head_dim);
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))
         return fail(PEVLM_ERR_WORKSPACE_TOO_SMALL, "cache attention workspace needs %zu bytes, 256-byte aligned (got %zu)",
@@ -226,7 +231,7 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
     p.n_q_heads = heads->n_q_heads;
     p.part_ml = (float *)workspace;
     // no request is longer than its row of the table
-    const int64_t longest = ceil_div(ceil_div(cache->max_pages * cache->page_size, kKv4Step), p.min_steps);
+    const int64_t longest = ceil_div(ceil_div(cache->max_pages * cache->page_size, kKv4Record << p.step_shift), p.min_steps);
     p.grid = (int32_t)std::min<int64_t>(p.max_items, p.max_units * longest);
     p.part_acc = (float *)((char *)workspace + ml_bytes(p));
     p.c_log2 = scale_of(heads) * 1.4426950408889634f;

@@ -1,0 +1,194 @@
+// Where a workgroup's item of the cache attention lies, and what it writes: shared by the kernels over the 4-bit cache.
+#pragma once
+#include "bf16_device.h"
+#include "kv4.h"
+#include "wave_scan.h"
+
+namespace pevlm {
+
+constexpr int32_t kMany = 0x3fffffff;  // two of them fit 31 bits
+
+// What a request's rows see: records (16 tokens) [0, n_sink) and [near, near + n_near), which do not overlap
+struct Span {
+    int32_t n_sink, near, records;
+};
+
+struct Request {
+    int32_t row0, rows, held, sink;  // rows: 0 if it has none (to write)
+    int32_t window;                  // < 0: none
+};
+
+__device__ __forceinline__ Request read_request(const Kv4Attn &p, int32_t s)
+{
+    Request r;
+    const int32_t width = p.max_pages << p.pool.page_shift;  // below 2^31
+    r.row0 = p.row_start[s];
+    r.rows = p.row_len[s];
+    const int32_t len = p.seq_len[s];
+    r.window = p.window ? p.window[s] : -1;
+    r.sink = p.window && p.sink_len ? p.sink_len[s] : 0;
+    r.held = len < 0 ? 0 : (len < width ? len : width);
+    if (r.window < 0) r.sink = 0;
+    r.sink = r.sink < 0 ? 0 : (r.sink < r.held ? r.sink : r.held);
+    if (r.row0 < 0 || r.rows < 0 || r.rows > p.num_rows - r.row0) r.rows = 0;
+    return r;
+}
+
+// First token inside the window of the token at position `pos`.  (Where the difference wraps, pos is negative and nothing is seen.)
+__device__ __forceinline__ int32_t near_of(const Request &r, int32_t pos)
+{
+    const int32_t n = (int32_t)((uint32_t)pos - (uint32_t)r.window + 1u);
+    return r.window < 0 || n < 0 ? 0 : (n < r.held ? n : r.held);
+}
+
+__device__ __forceinline__ Span span_of(const Request &r)
+{
+    Span s;
+    const int32_t first = near_of(r, r.held - r.rows);  // of the earliest row; a row before the first token sees nothing
+    s.n_sink = ceil_div(r.sink, kKv4Record);
+    s.near = first / kKv4Record;
+    if (s.near < s.n_sink) s.near = s.n_sink;
+    const int32_t end = ceil_div(r.held, kKv4Record);
+    s.records = s.n_sink + (first < r.held && end > s.near ? end - s.near : 0);
+    return s;
+}
+
+__device__ __forceinline__ int32_t steps_of(const Kv4Attn &p, const Span &s) { return (s.records + (1 << p.step_shift) - 1) >> p.step_shift; }
+
+__device__ __forceinline__ int32_t lane_value(int32_t x, int32_t lane) { return __builtin_amdgcn_readlane(x, lane); }
+// a value that is the same in every lane, where the compiler is to know it
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// x / d and the rest of it, x >= 0, d > 0.  Up to 2^20 in fp32: (x + 1/2) / d is at least 1 / (2 d) away from a whole number, and two
+// roundings move it by less.  (A whole-number division is some 40 instructions in a row, and a workgroup makes several before its first load.)
+__device__ __forceinline__ int32_t divide(int32_t x, int32_t d, int32_t &rest)
+{
+    const int32_t n = x < (1 << 20) ? (int32_t)(((float)x + 0.5f) * __builtin_amdgcn_rcpf((float)d)) : x / d;
+    rest = x - n * d;
+    return n;
+}
+__device__ __forceinline__ int32_t divide(int32_t x, int32_t d)
+{
+    int32_t rest;
+    return divide(x, d, rest);
+}
+__device__ __forceinline__ int32_t divide_up(int32_t x, int32_t d) { return divide(x + d - 1, d); }  // x + d below 2^31
+
+// Where the idx-th item (or unit) of a call lies.  Every wavefront finds its own by itself: lane by lane over 64 requests at a
+// time, once for the whole work, which sets the items' length, and once for the place.
+struct Place {
+    int32_t s, first_item, splits, tiles, rest;  // rest: the item's (unit's) place within the request
+    Request r;
+};
+
+template <bool UNITS>
+__device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
+{
+    const int32_t lane = threadIdx.x & 63;
+    Request r;
+    int32_t steps = 0, tiles = 0;
+    const auto look = [&](int32_t s) {
+        steps = tiles = 0;
+        if (s < p.num_seqs) {
+            r = read_request(p, s);
+            if (r.rows > 0) {
+                tiles = (r.rows * p.group + (1 << p.tile_shift) - 1) >> p.tile_shift;  // below 2^31: the host has looked at num_rows * group
+                steps = steps_of(p, span_of(r));
+            }
+        }
+    };
+    // Counts stop at kMany: with row ranges that overlap they can pass any bound, and no item or unit lies there
+    const auto count = [&](int32_t n) {
+        const float x = (float)n * (float)tiles * (float)p.pool.n_kv_heads;
+        return x < (float)kMany ? n * tiles * p.pool.n_kv_heads : kMany;
+    };
+    const auto sum = [](int32_t a, int32_t b) { return min(a + b, kMany); };
+    const auto total = [](auto x) { return __builtin_bit_cast(decltype(x), lane_value(__builtin_bit_cast(int32_t, x), 63)); };
+    // An item's steps: rounded up, all units of them make at most work / length + units items, which is to be p.target.  (What the sums
+    // round off is less than one part in 2^18, and max_items has room for that.)
+    float work = 0.f, units = 0.f;
+    const auto plus = [](float a, float b) { return a + b; };
+    for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
+        look(s0 + lane);
+        work += total(wave_scan((float)steps * (float)tiles, plus));
+        units += total(wave_scan((float)tiles, plus));
+    }
+    const float heads = (float)p.pool.n_kv_heads, room = (float)p.target - units * heads;
+    const float length = work * heads * __builtin_amdgcn_rcpf(room > 0.5f * p.target ? room : 0.5f * p.target);
+    const int32_t per = length < (float)p.min_steps ? p.min_steps : (length < 1e9f ? (int32_t)length + 1 : 1000000000);
+    const auto splits_of = [&] { return steps > per ? divide_up(steps, per) : 1; };  // rows that see nothing are an item, too
+
+    Place at;
+    at.s = -1;
+    at.first_item = 0;
+    if (!UNITS && p.by_xcd) {  // contiguous eighths of the items to the XCDs
+        int32_t all = 0;
+        for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
+            if (p.num_seqs > 64) look(s0 + lane);
+            all = sum(all, total(wave_scan(count(splits_of()), sum)));
+        }
+        all = all < p.max_items ? all : p.max_items;
+        const int32_t per_xcd = (all + 7) / 8, j = idx >> 3;
+        idx = (idx & 7) * per_xcd + j;
+        if (j >= per_xcd || idx >= all) return at;
+    }
+    int32_t before = 0;
+    for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
+        if (p.num_seqs > 64) look(s0 + lane);
+        const int32_t splits = splits_of(), items = count(splits), mine = UNITS ? count(1) : items;
+        const int32_t end = wave_scan(mine, sum), item_end = UNITS ? wave_scan(items, sum) : end;
+        const uint64_t found = __ballot(sum(before, end) > idx);
+        if (found) {
+            const int32_t f = __builtin_ctzll(found);
+            at.s = s0 + f;
+            at.rest = idx - before - (lane_value(end, f) - lane_value(mine, f));
+            at.splits = lane_value(splits, f);
+            at.tiles = lane_value(tiles, f);
+            at.first_item = sum(at.first_item, lane_value(item_end, f) - lane_value(items, f));
+            at.r.row0 = lane_value(r.row0, f);
+            at.r.rows = lane_value(r.rows, f);
+            at.r.held = lane_value(r.held, f);
+            at.r.sink = lane_value(r.sink, f);
+            at.r.window = lane_value(r.window, f);
+            return at;
+        }
+        before = sum(before, total(end));
+        at.first_item = sum(at.first_item, total(item_end));
+    }
+    return at;
+}
+
+// A KV head's query heads: as a map sorts them, or equal groups in order
+__device__ __forceinline__ int32_t first_head(const Kv4Attn &p, int32_t g) { return p.mapped ? p.heads.first[g] : g * p.group; }
+__device__ __forceinline__ int32_t heads_of(const Kv4Attn &p, int32_t g) { return p.mapped ? p.heads.first[g + 1] - p.heads.first[g] : p.group; }
+__device__ __forceinline__ int32_t query_head(const Kv4Attn &p, int32_t i) { return p.mapped ? p.heads.order[i] : i; }
+
+__device__ __forceinline__ uint16_t bf16_nearest(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
+
+// Four elements of a pair's row, from the values and sum of its weights against reference M
+template <int D, bool BF16>
+__device__ __forceinline__ void store_pair(const Kv4Attn &p, int64_t to, int32_t d4, f32x4 acc, float M, float l)
+{
+    const bool none = M == -INFINITY && l == 0.f;  // a row that sees nothing
+    acc = none ? f32x4{0.f, 0.f, 0.f, 0.f} : acc * (1.f / l);
+    if constexpr (BF16) {
+        const ushort4 x = make_ushort4(bf16_nearest(acc[0]), bf16_nearest(acc[1]), bf16_nearest(acc[2]), bf16_nearest(acc[3]));
+        *reinterpret_cast<ushort4 *>((uint16_t *)p.out + to * D + d4) = x;
+    } else {
+        *reinterpret_cast<f32x4 *>((float *)p.out + to * D + d4) = acc;
+    }
+    if (p.lse && d4 == 0) p.lse[to] = none ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+// A pair's part of a unit that was cut
+template <int D>
+__device__ __forceinline__ void store_part(const Kv4Attn &p, int64_t slot, int32_t d4, f32x4 acc, float M, float l)
+{
+    *reinterpret_cast<f32x4 *>(p.part_acc + slot * D + d4) = acc;
+    if (d4 == 0) {
+        p.part_ml[slot * 2] = M;
+        p.part_ml[slot * 2 + 1] = l;
+    }
+}
+
+}  // namespace pevlm

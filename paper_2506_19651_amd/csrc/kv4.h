@@ -60,11 +60,10 @@ struct Kv4Rows {  // rows of K and V that go into slots, or come out of them
     Kv4Pool pool;
 };
 
-// Attention.  A KV head's (row, query head) pairs of a request, head fastest, are cut into tiles of kKv4Pairs; a unit is one tile
-// against all keys that the request's rows see, in steps of kKv4Step tokens.  Units are cut into items of about equal
-// length: a workgroup takes an item.
-constexpr int32_t kKv4Pairs = 16;
-constexpr int32_t kKv4Step = 32;
+// Attention.  A KV head's (row, query head) pairs of a request, head fastest, are cut into tiles; a unit is one tile against all keys that
+// the request's rows see, in steps of a few records.  Units are cut into items of about equal length: a workgroup takes an item.
+constexpr int32_t kKv4TileShift = 4, kKv4StepShift = 1;          // 16 pairs, 2 records: the kernel of few rows
+constexpr int32_t kKv4RowsTileShift = 7, kKv4RowsStepShift = 2;  // 128 pairs, 4 records: of many
 
 struct Kv4Heads {
     uint8_t order[kMaxHeads];         // query heads sorted by KV head
@@ -79,12 +78,12 @@ struct Kv4Attn {
     const int32_t *table, *row_start, *row_len, *seq_len, *sink_len, *window;
     float *part_acc, *part_ml;        // [item][tile_pairs][D], [item][tile_pairs][2]: of items that are not whole units
     int32_t num_seqs, max_pages, num_rows, n_q_heads;
-    int32_t tile_pairs;               // pairs that a tile can have: kKv4Pairs, or all that the rows make
+    int32_t tile_shift, step_shift;   // pairs of a tile, records of a step
+    int32_t tile_pairs;               // pairs that a tile can have: all of a tile, or all that the rows make
     int32_t group;                    // query heads of the KV head that has most
     int32_t mapped;                   // whether a head map is given
     int32_t by_xcd;                   // whether an XCD takes neighbouring items, as tiles of the same keys are
-    float target_rcp;                 // 1 / items that a call is cut into, if they are not
-    int32_t min_steps;                // shorter than this
+    int32_t target, min_steps;        // items that a call is cut into, if they are not shorter than this
     int32_t max_items, max_units;     // bounds that no lengths pass
     int32_t grid;                     // and one for the items that the table's width allows
     float c_log2;                     // softmax scale * log2(e)
@@ -94,6 +93,7 @@ struct Kv4Attn {
 hipError_t launch_kv4_slots(const Kv4Slots &p, hipStream_t stream);
 hipError_t launch_kv4_store(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream);
 hipError_t launch_kv4_load(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream);
+void launch_attn_kv4_rows(const Kv4Attn &p, int32_t D, hipStream_t stream);  // bf16 tensors
 hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, bool merge, hipStream_t stream);
 
 }  // namespace pevlm
