@@ -180,6 +180,14 @@ __device__ __forceinline__ void store_pair(const Kv4Attn &p, int64_t to, int32_t
     if (p.lse && d4 == 0) p.lse[to] = none ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+// Where the 16-byte chunk c of a row of V lies in LDS.  Neighbouring rows lie in other banks both for the lanes that write a chunk of 8 rows
+// each and for those that read 32 bytes of 4 rows to transpose them.
+template <int D>
+__device__ __forceinline__ int32_t value_chunk(int32_t row, int32_t c)
+{
+    return c ^ ((row & (D / 16 - 1)) << 1);
+}
+
 // A pair's part of a unit that was cut
 template <int D>
 __device__ __forceinline__ void store_part(const Kv4Attn &p, int64_t slot, int32_t d4, f32x4 acc, float M, float l)

@@ -46,7 +46,6 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
     constexpr int DT = D / 16;         // tiles of 16 elements of an output row
     constexpr int NQ = BF16 ? 1 : 3, NP = BF16 ? 2 : 3;
     constexpr int ROWB = 2 * D;        // bytes of a V row in LDS
-    constexpr int CH = ROWB / 16;      // its 16-byte chunks
     constexpr int WORDS = D / 32;      // words of codes of a lane: 32 (16) elements of D = 128 (64)
     static_assert(WORDS == KS, "a lane's word is its share of a k-step");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[NW * 32 * ROWB];
@@ -203,7 +202,7 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
                 }
             }
         }
-        // ---- V rows to LDS: chunk c of row t lies at c ^ (t % CH)
+        // ---- V rows to LDS
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const float scale = kv4_scale(v_scale[e]);
@@ -214,7 +213,7 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
                 kv4_decode8(st.v[e][w], scale, x);
                 const uint4 four = make_uint4(__builtin_bit_cast(uint32_t, x[0]), __builtin_bit_cast(uint32_t, x[1]), __builtin_bit_cast(uint32_t, x[2]),
                                               __builtin_bit_cast(uint32_t, x[3]));
-                *reinterpret_cast<uint4 *>(slice + t * ROWB + (((kg * WORDS + w) ^ (l16 & (CH - 1))) << 4)) = four;
+                *reinterpret_cast<uint4 *>(slice + t * ROWB + value_chunk<D>(l16, kg * WORDS + w) * 16) = four;
             }
         }
         // ---- weights against the pair's reference, which is raised where a score outgrows it
@@ -249,7 +248,7 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int32_t tr = kg * 4 + (l16 >> 2);
-                const uint8_t *src = slice + (e * 16 + tr) * ROWB + (((t * 2 + ((l16 & 3) >> 1)) ^ (tr & (CH - 1))) << 4) + (l16 & 1) * 8;
+                const uint8_t *src = slice + (e * 16 + tr) * ROWB + value_chunk<D>(tr, t * 2 + ((l16 & 3) >> 1)) * 16 + (l16 & 1) * 8;
                 const bf16x4 four = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, src)));
                 a[e * 4] = four[0]; a[e * 4 + 1] = four[1]; a[e * 4 + 2] = four[2]; a[e * 4 + 3] = four[3];
             }
