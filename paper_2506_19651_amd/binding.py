@@ -524,10 +524,13 @@ def pevlm_visible_pairs(layout: Layout):
 
 
 # ------------------------------------------------------------------------------------------ paged KV cache in 4 bits
-_TORCH = None  # (torch, {dtype code: torch dtype}, current_device, raw stream of a device)
+# A step of generation makes these calls once a layer, and its kernels take as long as their checks: those are made in one loop
+# over the tensors, and the message is put together only where one fails.
+_TORCH = None
 
 
 def _torch():
+    """(torch.int32, {dtype code: torch dtype}, torch.float32, torch.uint8, the current device, a device's current raw stream)."""
     global _TORCH
     if _TORCH is None:
         import torch
@@ -535,7 +538,7 @@ def _torch():
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is None:
             raw = lambda device: torch.cuda.current_stream(device).cuda_stream  # noqa: E731
-        _TORCH = (torch, {PEVLM_F32: torch.float32, PEVLM_BF16: torch.bfloat16}, torch.cuda.current_device, raw)
+        _TORCH = (torch.int32, {PEVLM_F32: torch.float32, PEVLM_BF16: torch.bfloat16}, torch.float32, torch.uint8, torch.cuda.current_device, raw)
     return _TORCH
 
 
@@ -548,11 +551,11 @@ class KvCache:
     new_pool makes it) and the requests' block table (device int32 [num_seqs][max_pages]).  Holds on to both tensors."""
 
     def __init__(self, pool, block_table, page_size: int):
-        torch = _torch()[0]
-        if pool.dtype != torch.uint8 or pool.dim() != 4 or not pool.is_contiguous() or pool.shape[2] * 16 != page_size or pool.shape[3] % 17:
+        int32, _dtypes, _f32, uint8, _current, _raw = _torch()
+        if pool.dtype != uint8 or pool.dim() != 4 or not pool.is_contiguous() or pool.shape[2] * 16 != page_size or pool.shape[3] % 17:
             _refuse(f"the pool must be a contiguous uint8 tensor [num_pages][Hkv][page_size / 16][17 * head_dim], got {tuple(pool.shape)} of "
                     f"{pool.dtype} for pages of {page_size}")
-        if block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous():
+        if block_table.dtype != int32 or block_table.dim() != 2 or not block_table.is_contiguous():
             _refuse("block_table must be a contiguous int32 tensor [num_seqs][max_pages]")
         if pool.device != block_table.device:
             _refuse("the pool and block_table are on different devices")
@@ -565,7 +568,8 @@ class KvCache:
 
     @staticmethod
     def new_pool(heads: "Heads", num_pages: int, page_size: int, device):
-        torch = _torch()[0]
+        import torch
+
         if pevlm_cache_pool_bytes(heads, num_pages, page_size) == 0:
             _refuse(pevlm_last_error())
         return torch.zeros((num_pages, heads.n_kv_heads, page_size // 16, 17 * heads.head_dim), dtype=torch.uint8, device=device)
@@ -574,37 +578,60 @@ class KvCache:
         return self._ref
 
 
-class _Call:
-    """What a call on a cache checks of its tensors, and the device and stream that it runs on."""
-
-    def __init__(self, cache: KvCache):
-        self.device = cache.device
-        self.torch, self.dtypes, self.current, self.raw = _torch()
-
-    def ints(self, name, t, count, optional=False):
-        """Address of a contiguous int32 array of `count` entries."""
+def _arrays(cache: KvCache, int32, named):
+    """Addresses of contiguous int32 arrays on the cache's device: named = ((name, tensor, entries), ...); None may stand for an optional one."""
+    device, out = cache.device, []
+    for name, t, n in named:
         if t is None:
-            if not optional:
+            if name not in _OPTIONAL:
                 _refuse(f"{name} must be given")
-            return None
-        if t.dtype is not self.torch.int32 or t.numel() != count or not t.is_contiguous():
-            _refuse(f"{name} must be a contiguous int32 tensor of {count} entries, got {tuple(t.shape)} of {t.dtype}")
-        return self.here(name, t)
+            out.append(None)
+        else:
+            if t.dtype is not int32 or t.numel() != n or not t.is_contiguous():
+                _refuse(f"{name} must be a contiguous int32 tensor of {n} entries, got {tuple(t.shape)} of {t.dtype}")
+            if t.get_device() != device:
+                _refuse(f"{name} is on {t.device}, the cache on device {device}")
+            out.append(t.data_ptr())
+    return out
 
-    def here(self, name, t):
-        if t.get_device() != self.device:
-            _refuse(f"{name} is on {t.device}, the cache on device {self.device}")
-        return t.data_ptr()
 
-    def run(self, fn, args, stream):
-        """fn(*args, stream) on the cache's device."""
-        if self.device < 0:
-            _refuse("the cache is not in device memory")
-        if self.device == self.current():
-            _check(fn(*args, self.raw(self.device) if stream is None else _stream_ptr(stream)))
-            return
-        with self.torch.cuda.device(self.device):
-            _check(fn(*args, self.raw(self.device) if stream is None else _stream_ptr(stream)))
+_OPTIONAL = frozenset(("new_len", "pos_offset", "pos_ids", "sink_len", "window"))
+
+
+def _new_scratch(cache: KvCache, nbytes: int, stream):
+    """A workspace that belongs to the stream of the call: torch's allocator does not give its memory to other work before that stream is done."""
+    import torch
+
+    if cache.device < 0:
+        _refuse("the cache is not in device memory")
+    if stream is None:
+        return _workspace(nbytes, cache.pool)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream_ptr(stream), device=cache.device)
+    with torch.cuda.stream(stream):
+        return _workspace(nbytes, cache.pool)
+
+
+def _scratch(cache: KvCache, workspace):
+    if not workspace.is_contiguous() or workspace.get_device() != cache.device:
+        _refuse(f"the workspace must be contiguous and on the cache's device {cache.device}")
+    return workspace.data_ptr(), workspace.numel()
+
+
+def _on_device(cache: KvCache, fn, args, stream):
+    """fn(*args, stream) on the cache's device; stream None: torch's current one there."""
+    device, current, raw = cache.device, _TORCH[4], _TORCH[5]
+    if device < 0:
+        _refuse("the cache is not in device memory")
+    if device == current():
+        status = fn(*args, raw(device) if stream is None else _stream_ptr(stream))
+    else:
+        import torch
+
+        with torch.cuda.device(device):
+            status = fn(*args, raw(device) if stream is None else _stream_ptr(stream))
+    if status != PEVLM_OK:
+        _check(status)
 
 
 def _check_heads_of(cache: KvCache, heads: Heads):
@@ -623,45 +650,47 @@ def pevlm_cache_slots_workspace_bytes(num_seqs: int) -> int:
 def pevlm_cache_slots(cache: KvCache, seq_len, new_len, free_pages, num_free, seq_len_out, num_free_out, row_start, row_len, slot_map,
                       pos_ids=None, pos_offset=None, workspace=None, stream=None):
     """Pages, slots and positions of the new tokens.  num_rows is slot_map's length; pos_ids: int32 [3][num_rows]."""
-    c, n, rows, free = _Call(cache), cache.num_seqs, slot_map.numel(), free_pages.numel()
-    args = [cache.ref(), c.ints("seq_len", seq_len, n), c.ints("new_len", new_len, n, True), c.ints("free_pages", free_pages, free), free,
-            c.ints("num_free", num_free, 1), rows, c.ints("pos_offset", pos_offset, n, True), c.ints("seq_len_out", seq_len_out, n),
-            c.ints("num_free_out", num_free_out, 1), c.ints("row_start", row_start, n), c.ints("row_len", row_len, n),
-            c.ints("slot_map", slot_map, rows), c.ints("pos_ids", pos_ids, 3 * rows, True)]
+    int32 = (_TORCH or _torch())[0]
+    n, rows, free = cache.num_seqs, slot_map.numel(), free_pages.numel()
+    held, new, pages, left, offset, held_out, left_out, start, length, slots, pos = _arrays(cache, int32, (
+        ("seq_len", seq_len, n), ("new_len", new_len, n), ("free_pages", free_pages, free), ("num_free", num_free, 1), ("pos_offset", pos_offset, n),
+        ("seq_len_out", seq_len_out, n), ("num_free_out", num_free_out, 1), ("row_start", row_start, n), ("row_len", row_len, n),
+        ("slot_map", slot_map, rows), ("pos_ids", pos_ids, 3 * rows)))
     if workspace is None:
-        workspace = _workspace(pevlm_cache_slots_workspace_bytes(n), slot_map)
-    c.run(load_library().pevlm_cache_slots, args + [c.here("workspace", workspace), workspace.numel()], stream)
+        workspace = _new_scratch(cache, pevlm_cache_slots_workspace_bytes(n), stream)
+    ws, nbytes = _scratch(cache, workspace)
+    _on_device(cache, (_lib or load_library()).pevlm_cache_slots, (cache._ref, held, new, pages, free, left, rows, offset, held_out, left_out, start, length, slots,
+                                                         pos, ws, nbytes), stream)
     return workspace
 
 
-def _kv_rows(c: _Call, cache: KvCache, heads: Heads, rows: int, tensors):
-    """Addresses of k and v [rows][Hkv][D], whose rows may lie further apart, and their strides in elements."""
+def _kv_rows(cache: KvCache, heads: Heads, k, v, slot_map):
+    """Arguments of the calls that move rows: k and v [rows][Hkv][D], whose rows may lie further apart."""
     _check_heads_of(cache, heads)
-    dtype, inner = c.dtypes[heads.struct.dtype], cache.head_dim
-    shape, addresses, strides = (rows, cache.n_kv_heads, inner), [], []
-    for name, t in tensors:
+    int32, dtypes, _f32, _u8, _current, _raw = _TORCH or _torch()
+    rows, dtype, inner = slot_map.numel(), dtypes[heads.struct.dtype], cache.head_dim
+    shape, device, args = (rows, cache.n_kv_heads, inner), cache.device, []
+    for name, t in (("k", k), ("v", v)):
         if t.dtype is not dtype or t.shape != shape:
             _refuse(f"{name} must be {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
         stride = t.stride()
         if (stride[2] != 1 or (stride[1] != inner and shape[1] > 1)) and rows:
             _refuse(f"a row of {name} must be contiguous (strides {stride})")
-        addresses.append(c.here(name, t))
-        strides.append(stride[0] if rows > 1 else 0)
-    return addresses + strides
+        if t.get_device() != device:
+            _refuse(f"{name} is on {t.device}, the cache on device {device}")
+        args.append((t.data_ptr(), stride[0] if rows > 1 else 0))
+    (slots,) = _arrays(cache, int32, (("slot_map", slot_map, rows),))
+    return args[0][0], args[1][0], args[0][1], args[1][1], slots, rows, cache._ref, heads.ref()
 
 
 def pevlm_cache_store_kv4(k, v, slot_map, cache: KvCache, heads: Heads, stream=None):
     """k, v: [rows][Hkv][D] of the dtype of heads, rows contiguous in themselves; slot_map: int32 [rows]."""
-    c, rows = _Call(cache), slot_map.numel()
-    args = _kv_rows(c, cache, heads, rows, (("k", k), ("v", v)))
-    c.run(load_library().pevlm_cache_store_kv4, args + [c.ints("slot_map", slot_map, rows), rows, cache.ref(), heads.ref()], stream)
+    _on_device(cache, (_lib or load_library()).pevlm_cache_store_kv4, _kv_rows(cache, heads, k, v, slot_map), stream)
 
 
 def pevlm_cache_load_kv4(k, v, slot_map, cache: KvCache, heads: Heads, stream=None):
     """As pevlm_cache_store_kv4, the other way."""
-    c, rows = _Call(cache), slot_map.numel()
-    args = _kv_rows(c, cache, heads, rows, (("k", k), ("v", v)))
-    c.run(load_library().pevlm_cache_load_kv4, args + [c.ints("slot_map", slot_map, rows), rows, cache.ref(), heads.ref()], stream)
+    _on_device(cache, (_lib or load_library()).pevlm_cache_load_kv4, _kv_rows(cache, heads, k, v, slot_map), stream)
 
 
 def pevlm_cache_attn_workspace_bytes(heads: Heads, num_seqs: int, num_rows: int) -> int:
@@ -671,18 +700,25 @@ def pevlm_cache_attn_workspace_bytes(heads: Heads, num_seqs: int, num_rows: int)
 def pevlm_cache_attn_kv4(q, out, cache: KvCache, heads: Heads, row_start, row_len, seq_len, sink_len=None, window=None, lse=None,
                          workspace=None, stream=None):
     """q, out: contiguous [rows][Hq][D] of the dtype of heads; lse: float32 [rows][Hq] or None."""
-    c, n = _Call(cache), cache.num_seqs
     _check_heads_of(cache, heads)
-    shape, dtype = (q.shape[0], heads.n_q_heads, heads.head_dim), c.dtypes[heads.struct.dtype]
+    int32, dtypes, f32, _u8, _current, _raw = _TORCH or _torch()
+    n, rows, device = cache.num_seqs, q.shape[0], cache.device
+    shape, dtype = (rows, heads.n_q_heads, heads.head_dim), dtypes[heads.struct.dtype]
     for name, t in (("q", q), ("out", out)):
         if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-            _refuse(f"{name} must be contiguous, [rows][{shape[1]}][{shape[2]}] of {dtype}, got {tuple(t.shape)} of {t.dtype}")
-    if lse is not None and (lse.dtype is not c.torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous()):
-        _refuse(f"lse must be contiguous, {shape[:2]} of float32, got {tuple(lse.shape)} of {lse.dtype}")
+            _refuse(f"{name} must be contiguous, {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+        if t.get_device() != device:
+            _refuse(f"{name} is on {t.device}, the cache on device {device}")
+    if lse is not None:
+        if lse.dtype is not f32 or lse.shape != shape[:2] or not lse.is_contiguous():
+            _refuse(f"lse must be contiguous, {shape[:2]} of {f32}, got {tuple(lse.shape)} of {lse.dtype}")
+        if lse.get_device() != device:
+            _refuse(f"lse is on {lse.device}, the cache on device {device}")
+    start, length, held, sink, near = _arrays(cache, int32, (("row_start", row_start, n), ("row_len", row_len, n), ("seq_len", seq_len, n),
+                                                             ("sink_len", sink_len, n), ("window", window, n)))
     if workspace is None:
-        workspace = _workspace(pevlm_cache_attn_workspace_bytes(heads, n, shape[0]), q)
-    args = [c.here("q", q), c.here("out", out), None if lse is None else c.here("lse", lse), cache.ref(), heads.ref(), shape[0],
-            c.ints("row_start", row_start, n), c.ints("row_len", row_len, n), c.ints("seq_len", seq_len, n),
-            c.ints("sink_len", sink_len, n, True), c.ints("window", window, n, True), c.here("workspace", workspace), workspace.numel()]
-    c.run(load_library().pevlm_cache_attn_kv4, args, stream)
+        workspace = _new_scratch(cache, pevlm_cache_attn_workspace_bytes(heads, n, rows), stream)
+    ws, nbytes = _scratch(cache, workspace)
+    _on_device(cache, (_lib or load_library()).pevlm_cache_attn_kv4, (q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), cache._ref,
+                                                                        heads.ref(), rows, start, length, held, sink, near, ws, nbytes), stream)
     return workspace
