@@ -336,7 +336,7 @@ typedef struct {
     int32_t num_pages;          /* >= 1; num_pages * page_size below 2^31 */
     int32_t page_size;          /* tokens of a page: a power of two from 16 to 4096 */
     int32_t num_seqs;           /* >= 1 requests */
-    int32_t max_pages;          /* >= 1 columns of the table; max_pages * page_size below 2^31 */
+    int32_t max_pages;          /* >= 1 columns of the table; max_pages * page_size at most 2^30 */
     int32_t *block_table;       /* DEVICE [num_seqs][max_pages] */
 } pevlm_cache;
 

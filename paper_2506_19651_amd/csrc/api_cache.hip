@@ -9,9 +9,7 @@
 namespace pevlm {
 
 constexpr int32_t kMinPage = 16, kMaxPage = 4096;
-
-// Pairs of (row, query head) of a KV head and request, on average, above which the kernel of many rows is taken
-constexpr int64_t kManyPairs = 48;
+constexpr int32_t kMaxTokens = 1 << 30;  // of a request: a token's place and a tile's length add up in 32 bits
 
 static bool page_size_ok(int32_t n) { return n >= kMinPage && n <= kMaxPage && (n & (n - 1)) == 0; }
 
@@ -38,8 +36,8 @@ static pevlm_status check_pool_memory(const pevlm_cache *c)
 
 static pevlm_status check_table(const pevlm_cache *c)
 {
-    if (c->num_seqs < 1 || c->max_pages < 1 || (int64_t)c->max_pages * c->page_size > INT32_MAX)
-        return fail(PEVLM_ERR_INVALID_ARG, "block table [%d][%d] of pages of %d tokens: need >= 1 request, >= 1 column and fewer than 2^31 tokens a request",
+    if (c->num_seqs < 1 || c->max_pages < 1 || (int64_t)c->max_pages * c->page_size > kMaxTokens)
+        return fail(PEVLM_ERR_INVALID_ARG, "block table [%d][%d] of pages of %d tokens: need >= 1 request, >= 1 column and at most 2^30 tokens a request",
                     c->num_seqs, c->max_pages, c->page_size);
     if (!c->block_table || !aligned4(c->block_table)) return fail(PEVLM_ERR_INVALID_ARG, "block_table must be a 4-byte aligned device pointer");
     return PEVLM_OK;
@@ -85,20 +83,36 @@ static int32_t group_heads(const HeadTable &tab, const pevlm_heads *h, Kv4Heads 
     return most;
 }
 
+// Whether the kernel of many rows is taken: by the tiles of 16 and of 128 that a request's (row, query head) pairs of a KV head fill, on average.  A
+// tile of 128 takes the time of four of 16, of 64-wide heads of seven.  One request of 65.9 K tokens, 16 / 128: 28/4 heads x 128, 7 rows 33.8 / 34.6 us,
+// 14 rows 47.1 / 41.0, 20 rows 55.1 / 55.7, 40 rows 96 / 72, 128 rows 282 / 145; 32/8 heads 14 rows 49.6 / 50.4, 28 rows 78 / 59; 14/2 heads x 64, 18
+// rows 26.8 / 28.5, 128 rows 92 / 66.  Up to a few thousand tokens its start and longer steps do not pay (2000 tokens x 28/4, 14 rows 14.8 / 17.9, 60
+// rows 21.0 / 24.4, 128 rows 28.3 / 28.1): how long a request is stands on the GPU, the table's width is looked at.
+constexpr int64_t kManyRowsTokens = 4096;
+static bool many_rows(const pevlm_heads *h, int32_t group, int32_t num_seqs, int32_t num_rows, int64_t width)
+{
+    if (h->dtype != PEVLM_BF16 || width < kManyRowsTokens) return false;
+    const int64_t asking = std::max(1, std::min(num_seqs, num_rows)), pairs = ((int64_t)num_rows * group + asking - 1) / asking;
+    return (pairs + 15) / 16 > (h->head_dim == 128 ? 4 : 7) * ((pairs + 127) / 128);
+}
+
 // What bounds a call's items, and how it is cut.  A request with r rows has ceil(r * group / tile) tiles of a KV head.
-static void size_attn(const pevlm_heads *h, int32_t num_seqs, int32_t num_rows, Kv4Attn *p)
+static void size_attn(const pevlm_heads *h, int32_t num_seqs, int32_t num_rows, int64_t width, Kv4Attn *p)
 {
     HeadTable tab;
     check_heads(h, &tab);
     p->group = group_heads(tab, h, &p->heads);
     p->mapped = h->kv_head_of_q != nullptr;
     const int64_t asking = std::max(1, std::min(num_seqs, num_rows)), pairs = (int64_t)num_rows * p->group;
-    const bool many = h->dtype == PEVLM_BF16 && pairs > kManyPairs * asking;
+    const bool many = many_rows(h, p->group, num_seqs, num_rows, width);
     p->tile_shift = many ? kKv4RowsTileShift : kKv4TileShift;
     p->step_shift = many ? kKv4RowsStepShift : kKv4StepShift;
     p->tile_pairs = (int32_t)std::min<int64_t>(1 << p->tile_shift, pairs);
-    p->target = (many ? 2 : 6) * compute_units();
-    p->min_steps = many ? 8 : 12;
+    // workgroups that a compute unit holds at a time: a call is one round of them.  (Two rounds of shorter items are 3 % slower, 16 requests of
+    // 65.9 K tokens 116.5 -> 119.4 us, four 8 %: an item's start and end, some 6 us, come twice.)
+    const int32_t resident = many ? 2 : (h->head_dim == 64 ? 4 : (h->dtype == PEVLM_BF16 ? 3 : 2));
+    p->target = resident * compute_units();
+    p->min_steps = many ? 4 : 12;
     p->by_xcd = pairs > asking << p->tile_shift;
     const int64_t units = h->n_kv_heads * (asking + (pairs >> p->tile_shift));
     p->max_units = (int32_t)std::min<int64_t>(units, INT32_MAX);
@@ -195,8 +209,12 @@ size_t pevlm_cache_attn_workspace_bytes(const pevlm_heads *heads, int32_t num_se
         return 0;
     }
     Kv4Attn p;
-    size_attn(heads, num_seqs, num_rows, &p);
-    return attn_bytes(p, heads->head_dim) + 256;
+    size_t bytes = 0;
+    for (int64_t width : {(int64_t)0, kManyRowsTokens}) {  // a call is cut one way or the other by its table
+        size_attn(heads, num_seqs, num_rows, width, &p);
+        bytes = std::max(bytes, attn_bytes(p, heads->head_dim));
+    }
+    return bytes + 256;
 }
 
 pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pevlm_cache *cache, const pevlm_heads *heads, int32_t num_rows,
@@ -216,7 +234,7 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
     if (!row_start || !row_len || !seq_len) return fail(PEVLM_ERR_INVALID_ARG, "row_start, row_len and seq_len must not be NULL");
     for (const int32_t *a : {row_start, row_len, seq_len, sink_len, window, (const int32_t *)lse})
         if (!aligned4(a)) return fail(PEVLM_ERR_INVALID_ARG, "arrays must be 4-byte aligned");
-    size_attn(heads, cache->num_seqs, num_rows, &p);
+    size_attn(heads, cache->num_seqs, num_rows, (int64_t)cache->max_pages * cache->page_size, &p);
     if (p.max_items > 0x3fffffff || ((int64_t)p.max_units << p.tile_shift) > INT32_MAX) return fail(PEVLM_ERR_UNSUPPORTED, "too many work items");
     const size_t need = attn_bytes(p, heads->head_dim);
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))

@@ -104,8 +104,9 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
     };
     const auto sum = [](int32_t a, int32_t b) { return min(a + b, kMany); };
     const auto total = [](auto x) { return __builtin_bit_cast(decltype(x), lane_value(__builtin_bit_cast(int32_t, x), 63)); };
-    // An item's steps: rounded up, all units of them make at most work / length + units items, which is to be p.target.  (What the sums
-    // round off is less than one part in 2^18, and max_items has room for that.)
+    // An item's steps.  The items of all units are to be p.target: at least work / target steps; with work / (target - units) it cannot be
+    // passed, whatever is lost to rounding up.  The shortest of those two and the length between them that keeps to it is taken (up to 64 requests, which
+    // the lanes hold; others take the last).  What the sums round off is less than one part in 2^18, and max_items has room for that.
     float work = 0.f, units = 0.f;
     const auto plus = [](float a, float b) { return a + b; };
     for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
@@ -113,9 +114,20 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
         work += total(wave_scan((float)steps * (float)tiles, plus));
         units += total(wave_scan((float)tiles, plus));
     }
-    const float heads = (float)p.pool.n_kv_heads, room = (float)p.target - units * heads;
-    const float length = work * heads * __builtin_amdgcn_rcpf(room > 0.5f * p.target ? room : 0.5f * p.target);
-    const int32_t per = length < (float)p.min_steps ? p.min_steps : (length < 1e9f ? (int32_t)length + 1 : 1000000000);
+    const float heads = (float)p.pool.n_kv_heads, target = (float)p.target, room = target - units * heads;
+    const auto length = [&](float items) {
+        const float x = work * heads * __builtin_amdgcn_rcpf(items);
+        return max(p.min_steps, x < 1e9f ? (int32_t)x + 1 : 1000000000);
+    };
+    int32_t per = length(room > 0.5f * target ? room : 0.5f * target);
+    if (p.num_seqs <= 64) {
+        const int32_t least = length(target);
+        const auto keeps = [&](int32_t n) {
+            const float all = total(wave_scan((float)(steps > n ? divide_up(steps, n) : 1) * (float)tiles, plus));
+            return all * heads <= target;
+        };
+        if (per > least) per = keeps(least) ? least : (keeps((least + per) / 2) ? (least + per) / 2 : per);
+    }
     const auto splits_of = [&] { return steps > per ? divide_up(steps, per) : 1; };  // rows that see nothing are an item, too
 
     Place at;

@@ -427,9 +427,11 @@ static void launch(const Kv4Attn &p, bool merge, hipStream_t stream)
     if (p.tile_shift == kKv4RowsTileShift) launch_attn_kv4_rows(p, D, stream);
     else hipLaunchKernelGGL((attn_kv4_kernel<D, BF16>), dim3((p.grid + 7) / 8 * 8), dim3(NW * 64), 0, stream, p);
     if (!merge) return;
-    // few units are cut into many items
-    if (p.max_units <= 16) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16>), dim3(p.max_units * p.tile_pairs), dim3(1024), 0, stream, p);
-    else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 2>), dim3(p.max_units * ceil_div(p.tile_pairs, 2)), dim3(256), 0, stream, p);
+    // few units are cut into many items, whose joining is worth more wavefronts where there are few pairs
+    const bool long_units = p.max_units <= 16;
+    if (!long_units) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 2>), dim3(p.max_units * ceil_div(p.tile_pairs, 2)), dim3(256), 0, stream, p);
+    else if (p.tile_pairs > kKv4Pairs) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 4>), dim3(p.max_units * p.tile_pairs), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16>), dim3(p.max_units * p.tile_pairs), dim3(1024), 0, stream, p);
 }
 
 hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, bool merge, hipStream_t stream)
