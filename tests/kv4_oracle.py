@@ -150,8 +150,9 @@ def attention(q, pool, table, kv_of_q, row_start, row_len, seq_len, sink_len=Non
             if not seen.any():
                 r["out"][row], r["lse"][row] = 0, -np.inf
                 continue
+            of = {g: (k[seen, g], v[seen, g]) for g in set(kv_of_q)}
             for h in range(hq):
-                kk, vv = k[seen, kv_of_q[h]], v[seen, kv_of_q[h]]
+                kk, vv = of[kv_of_q[h]]
                 x = kk @ q[row, h].astype(np.float64) * scale
                 top = x.max()
                 w = np.exp(x - top)

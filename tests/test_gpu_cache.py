@@ -185,11 +185,13 @@ def test_slots_of_many_requests(n):
 
 
 # ------------------------------------------------------------------------------------------ attention
-def attn_case(hq, hkv, d, dtype, page, lengths, rows, sink=None, window=None, kv_of_q=None, scale=0.0, seed=0, order=None, edit=None, q_scale=1.0):
-    """Makes a cache and queries, calls, and holds out and lse to the oracle.  order: row_start of every request (default: packed)."""
+def attn_case(hq, hkv, d, dtype, page, lengths, rows, sink=None, window=None, kv_of_q=None, scale=0.0, seed=0, order=None, edit=None, q_scale=1.0,
+              wide=False):
+    """Makes a cache and queries, calls, and holds out and lse to the oracle.  order: row_start of every request (default: packed); wide: a
+    table of 4096 tokens a request and more, so that with as many (row, head) pairs the kernel of many rows is taken."""
     rng = np.random.default_rng(seed + hq + d)
     heads = P.Heads(hq, hkv, d, dtype, kv_of_q, scale)
-    table, pages = pages_for([max(n, 0) for n in lengths], page, rng)
+    table, pages = pages_for([max(n, 0) for n in lengths], page, rng, width=max(-(-max(lengths) // page), 4096 // page) if wide else None)
     pool = np.zeros((pages, hkv, page // 16, 17 * d), np.uint8)
     for s, n in enumerate(lengths):
         j = np.arange(max(n, 0))
@@ -209,6 +211,10 @@ def attn_case(hq, hkv, d, dtype, page, lengths, rows, sink=None, window=None, kv
     if edit:
         edit(a)
         q, q64 = q[:a["num_rows"]].contiguous(), q64[:a["num_rows"]]
+    if wide:
+        group = max(np.bincount(kv_of_q)) if kv_of_q is not None else hq // hkv
+        pairs = -(-len(q) * group // min(len(rows), len(q)))
+        assert dtype == "bf16" and -(-pairs // 16) > (4 if d == 128 else 7) * -(-pairs // 128)
     cache = P.KvCache(torch.from_numpy(a["pool"]).to(DEV), i32(a["table"]), page)
     out = torch.full_like(q, 5.0)
     lse = torch.full(q.shape[:2], 5.0, device=DEV)
@@ -340,9 +346,9 @@ def test_bad_pages_and_lengths(rows, dtype):
     attn_case(8, 2, 64, dtype, 16, [96, 90, 33], rows, edit=negative)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows", [[1, 1], [3, 40]])
-def test_blocks_without_a_value(rows, dtype):
+@pytest.mark.parametrize("dtype,rows,wide", [("bf16", [1, 1], False), ("f32", [1, 1], False), ("bf16", [3, 40], False), ("f32", [3, 40], False),
+                                             ("bf16", [3, 40], True), ("bf16", [19, 47], True)])
+def test_blocks_without_a_value(dtype, rows, wide):
     """NaN blocks reach the rows that see them: a key's all of the row, a value's its 32 elements; masked ones nobody."""
     def nan_at(a, s, token, which, block):
         slot = a["table"][s, token // 16] * 16 + token % 16
@@ -360,15 +366,89 @@ def test_blocks_without_a_value(rows, dtype):
         nan_at(a, 0, 31, 0, 3)
     lengths = [120, 50]
     first = [120 - rows[0], 50 - rows[1]]
-    want = attn_case(4, 1, 128, dtype, 16, lengths, rows, edit=value)
+    want = attn_case(4, 1, 128, dtype, 16, lengths, rows, edit=value, wide=wide)
     assert np.isnan(want["out"][0][:, 64:96]).all() and np.isfinite(want["out"][0][:, :64]).all()
-    want = attn_case(4, 1, 128, dtype, 16, lengths, rows, edit=key)
+    want = attn_case(4, 1, 128, dtype, 16, lengths, rows, edit=key, wide=wide)
     assert np.isnan(want["out"][0]).all() and np.isfinite(want["out"][rows[0]:]).all()
-    want = attn_case(4, 1, 128, dtype, 16, lengths, rows, sink=[29, 0], window=[first[0] - 31, -1], edit=hidden)
+    want = attn_case(4, 1, 128, dtype, 16, lengths, rows, sink=[29, 0], window=[first[0] - 31, -1], edit=hidden, wide=wide)
     assert np.isfinite(want["out"]).all()
     # a value that some rows of a question see and earlier ones do not
-    want = attn_case(4, 1, 128, dtype, 16, lengths, rows, edit=lambda a: nan_at(a, 1, 49, 1, 1))
+    want = attn_case(4, 1, 128, dtype, 16, lengths, rows, edit=lambda a: nan_at(a, 1, 49, 1, 1), wide=wide)
     assert np.isnan(want["out"][-1][:, 32:64]).all() and np.isfinite(want["out"][:-1]).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(28, 4, 128), (14, 2, 64), (3, 3, 64), (8, 8, 128), (33, 3, 64)])
+@pytest.mark.parametrize("page", [16, 64, 512])
+def test_many_rows(page, hq, hkv, d):
+    attn_case(hq, hkv, d, "bf16", page, [1500], [128], wide=True)
+    attn_case(hq, hkv, d, "bf16", page, [200, 119, 300, 135], [100, 119, 161, 129], wide=True)
+
+
+def test_many_rows_with_masks():
+    n = [200, 333, 64, 500, 90]
+    attn_case(8, 2, 128, "bf16", 16, n, [40, 64, 70, 33, 80], sink=[0, 16, 300, 5, -3], window=[0, 1, 16, 100, 2 ** 31 - 1], wide=True)
+    attn_case(8, 2, 128, "bf16", 16, n, [40, 64, 60, 33, 80], window=[-1, 50, 64, 65, 63], wide=True)
+    attn_case(14, 2, 64, "bf16", 32, [2500, 700], [77, 130], sink=[100, 17], window=[600, 1], wide=True)
+    want = attn_case(14, 2, 64, "bf16", 16, [30, 0, 320], [150, 2, 250], wide=True)  # more rows than tokens
+    assert (want["keys"][:120] == 0).all() and (want["keys"][150:152] == 0).all() and want["keys"][120] == 1
+
+
+def test_many_rows_of_mapped_heads():
+    attn_case(6, 3, 64, "bf16", 16, [150, 600], [100, 200], kv_of_q=[2, 0, 2, 2, 0, 2], wide=True)
+    attn_case(8, 2, 128, "bf16", 32, [300, 131], [60, 40], kv_of_q=[1, 0, 0, 1, 1, 0, 1, 0], wide=True)
+    attn_case(40, 2, 64, "bf16", 32, [100, 31], [20, 12], kv_of_q=[1] * 39 + [0], scale=0.2, wide=True)
+
+
+def test_many_rows_with_scores_far_apart():
+    attn_case(8, 2, 128, "bf16", 16, [400, 77], [60, 70], q_scale=12.0, wide=True)
+    attn_case(2, 1, 64, "bf16", 16, [1500], [127], scale=6.0, wide=True)
+
+
+def test_many_rows_of_a_padded_batch():
+    attn_case(4, 2, 64, "bf16", 16, [140, 0, 117, 190], [120, 0, 101, 77], order=[380, 360, 0, 200], wide=True)
+
+    def short(a):  # rows that end behind the tensors
+        a["num_rows"] = 499
+        a["row_start"][:] = [380, 360, 90, -1]
+    attn_case(4, 2, 64, "bf16", 16, [140, 0, 117, 190], [120, 0, 101, 77], order=[380, 360, 0, 200], edit=short, wide=True)
+
+
+def test_many_rows_with_bad_pages_and_lengths():
+    def edit(a):
+        a["table"][0, 2] = -1
+        a["table"][1, [0, 3]] = [len(a["pool"]), 2 ** 31 - 1]
+        a["table"][2, :] = -(2 ** 31)
+        a["seq_len"][0] = 2 ** 31 - 1  # as long as the table is wide
+    attn_case(8, 2, 128, "bf16", 16, [96, 90, 33], [40, 90, 60], edit=edit, wide=True)
+
+    def negative(a):
+        a["seq_len"][:] = [-5, 0, 212]
+        a["row_len"][1] = -(2 ** 31)
+    attn_case(8, 2, 128, "bf16", 16, [96, 90, 212], [40, 90, 60], edit=negative, wide=True)
+
+
+def test_many_requests_with_many_rows():
+    rng = np.random.default_rng(6)
+    attn_case(4, 1, 128, "bf16", 16, rng.integers(1, 100, 150).tolist(), rng.integers(20, 40, 150).tolist(), wide=True)
+
+
+def test_lengths_of_many_millions():
+    """Every page of the table is the same one: the rows before the last see n copies of its tokens, so out is that of one page and lse more by log(n)."""
+    page, width = 4096, 1 << 13  # 2^25 tokens
+    rng = np.random.default_rng(3)
+    for rows, d in ((1, 128), (1, 64), (130, 128), (130, 64)):
+        pool = np.zeros((1, 1, page // 16, 17 * d), np.uint8)
+        O.put(pool, np.arange(page), rng.standard_normal((page, 1, d)), rng.standard_normal((page, 1, d)))
+        q, q64 = rounded(rng.standard_normal((rows, 1, d)), "bf16")
+        heads = P.Heads(1, 1, d, "bf16")
+        cache = P.KvCache(torch.from_numpy(pool).to(DEV), torch.zeros((1, width), dtype=torch.int32, device=DEV), page)
+        out, lse = torch.empty_like(q), torch.empty((rows, 1), device=DEV)
+        P.pevlm_cache_attn_kv4(q, out, cache, heads, i32([0]), i32([rows]), i32([page * width]), lse=lse)
+        last = O.attention(q64[-1:], pool, np.array([[0]]), [0], [0], [1], [page])
+        got, got_lse = out[-1:].double().cpu().numpy(), lse[-1:].double().cpu().numpy()
+        n = page * width / 512 * U  # an item's tokens, of at least 512 items: its sums in fp32 are within n of them, relative to what they add up
+        assert (np.abs(got_lse - last["lse"] - np.log(width)) <= 2 * n + 1e-5).all()
+        assert (np.abs(got - last["out"]) <= 2.0 ** -8 * np.abs(last["out"]) + (2.0 ** -8 + 8 * n) * last["mass"]).all()
 
 
 def test_a_pool_beyond_32_bits():
@@ -382,7 +462,7 @@ def test_a_pool_beyond_32_bits():
     v, v64 = rounded(rng.standard_normal((600, 4, 128)), "bf16")
     table = np.array([[pages - 1, 3, pages // 2 + 7]])
     slots = table[0, np.arange(600) // page] * page + np.arange(600) % page
-    cache = P.KvCache(pool, i32(table), page)
+    cache = P.KvCache(pool, i32(np.pad(table, ((0, 0), (0, 13)))), page)
     P.pevlm_cache_store_kv4(k, v, i32(slots), cache, heads)
     back = torch.empty_like(k), torch.empty_like(v)
     P.pevlm_cache_load_kv4(*back, i32(slots), cache, heads)

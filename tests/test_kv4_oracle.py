@@ -110,7 +110,7 @@ def _cache(**changes):
 
 
 BAD_POOLS = [dict(page_size=8), dict(page_size=24), dict(page_size=8192), dict(num_pages=0), dict(num_pages=1 << 27)]
-BAD_TABLES = [dict(num_seqs=0), dict(max_pages=0), dict(max_pages=1 << 27), dict(block_table=None), dict(block_table=FAKE + 2)]
+BAD_TABLES = [dict(num_seqs=0), dict(max_pages=0), dict(max_pages=(1 << 26) + 1), dict(max_pages=1 << 27), dict(block_table=None), dict(block_table=FAKE + 2)]
 
 
 @pytest.mark.parametrize("changes", BAD_POOLS + [dict(pool=None), dict(pool=FAKE + 8)])
