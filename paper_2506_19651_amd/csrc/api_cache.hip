@@ -110,7 +110,7 @@ static void size_attn(const pevlm_heads *h, int32_t num_seqs, int32_t num_rows, 
     p->tile_pairs = (int32_t)std::min<int64_t>(1 << p->tile_shift, pairs);
     // workgroups that a compute unit holds at a time: a call is one round of them.  (Two rounds of shorter items are 3 % slower, 16 requests of
     // 65.9 K tokens 116.5 -> 119.4 us, four 8 %: an item's start and end, some 6 us, come twice.)
-    const int32_t resident = many ? 2 : (h->head_dim == 64 ? 4 : (h->dtype == PEVLM_BF16 ? 3 : 2));
+    const int32_t resident = many ? 2 : (h->head_dim == 64 ? 4 : 3);
     p->target = resident * compute_units();
     p->min_steps = many ? 4 : 12;
     p->by_xcd = pairs > asking << p->tile_shift;
@@ -235,7 +235,7 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
     for (const int32_t *a : {row_start, row_len, seq_len, sink_len, window, (const int32_t *)lse})
         if (!aligned4(a)) return fail(PEVLM_ERR_INVALID_ARG, "arrays must be 4-byte aligned");
     size_attn(heads, cache->num_seqs, num_rows, (int64_t)cache->max_pages * cache->page_size, &p);
-    if (p.max_items > 0x3fffffff || ((int64_t)p.max_units << p.tile_shift) > INT32_MAX) return fail(PEVLM_ERR_UNSUPPORTED, "too many work items");
+    if (p.max_items > 0x3fffffff || ((int64_t)p.max_units << p.tile_shift) > 1 << 30) return fail(PEVLM_ERR_UNSUPPORTED, "too many work items");
     const size_t need = attn_bytes(p, heads->head_dim);
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))
         return fail(PEVLM_ERR_WORKSPACE_TOO_SMALL, "cache attention workspace needs %zu bytes, 256-byte aligned (got %zu)",

@@ -21,7 +21,7 @@ struct Request {
 __device__ __forceinline__ Request read_request(const Kv4Attn &p, int32_t s)
 {
     Request r;
-    const int32_t width = p.max_pages << p.pool.page_shift;  // below 2^31
+    const int32_t width = p.max_pages << p.pool.page_shift;  // at most 2^30
     r.row0 = p.row_start[s];
     r.rows = p.row_len[s];
     const int32_t len = p.seq_len[s];
@@ -59,29 +59,46 @@ __device__ __forceinline__ int32_t lane_value(int32_t x, int32_t lane) { return 
 // a value that is the same in every lane, where the compiler is to know it
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// x / d and the rest of it, x >= 0, d > 0.  Up to 2^20 in fp32: (x + 1/2) / d is at least 1 / (2 d) away from a whole number, and two
-// roundings move it by less.  (A whole-number division is some 40 instructions in a row, and a workgroup makes several before its first load.)
+// x / d and the rest of it, 0 <= x < 2^30, 0 < d < 2^30, without a branch: an estimate that is within 2^8 (x / d to 2^-22 of it), what that leaves by
+// the same factor, to within one.  (The compiler's division is twice as long, in a chain of integer products, and a workgroup makes several
+// before its first load.)
 __device__ __forceinline__ int32_t divide(int32_t x, int32_t d, int32_t &rest)
 {
-    const int32_t n = x < (1 << 20) ? (int32_t)(((float)x + 0.5f) * __builtin_amdgcn_rcpf((float)d)) : x / d;
+    const float f = __builtin_amdgcn_rcpf((float)d);
+    int32_t n = (int32_t)((float)x * f);
     rest = x - n * d;
-    return n;
+    const int32_t more = (int32_t)__builtin_floorf((float)rest * f);
+    n += more;
+    rest -= more * d;
+    const int32_t under = rest < 0, over = rest >= d;
+    rest += under ? d : (over ? -d : 0);
+    return n + over - under;
 }
 __device__ __forceinline__ int32_t divide(int32_t x, int32_t d)
 {
     int32_t rest;
     return divide(x, d, rest);
 }
-__device__ __forceinline__ int32_t divide_up(int32_t x, int32_t d) { return divide(x + d - 1, d); }  // x + d below 2^31
+__device__ __forceinline__ int32_t divide_up(int32_t x, int32_t d) { return divide(x + d - 1, d); }  // x + d below 2^30
+
+// The call's fields, asked for together when a kernel begins.  The compiler asks for each where it is used, and waits there: ten waits in a row
+// before the first load of a record.
+__device__ __forceinline__ void have_fields(const Kv4Attn &p)
+{
+    asm volatile("" ::"s"(p.q), "s"(p.out), "s"(p.lse), "s"(p.pool.base), "s"(p.pool.num_pages), "s"(p.pool.page_shift), "s"(p.pool.n_kv_heads), "s"(p.table),
+                 "s"(p.row_start), "s"(p.row_len), "s"(p.seq_len), "s"(p.sink_len), "s"(p.window), "s"(p.part_acc), "s"(p.part_ml), "s"(p.num_seqs),
+                 "s"(p.max_pages), "s"(p.num_rows), "s"(p.n_q_heads), "s"(p.tile_pairs), "s"(p.group), "s"(p.mapped), "s"(p.by_xcd), "s"(p.target),
+                 "s"(p.min_steps), "s"(p.max_items), "s"(p.c_log2));
+}
 
 // Where the idx-th item (or unit) of a call lies.  Every wavefront finds its own by itself: lane by lane over 64 requests at a
-// time, once for the whole work, which sets the items' length, and once for the place.
+// time, once for the whole work, which sets the items' length, and once for the place.  FEW: up to 64 requests, which the lanes keep.
 struct Place {
     int32_t s, first_item, splits, tiles, rest;  // rest: the item's (unit's) place within the request
     Request r;
 };
 
-template <bool UNITS>
+template <bool UNITS, bool FEW>
 __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
 {
     const int32_t lane = threadIdx.x & 63;
@@ -92,7 +109,7 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
         if (s < p.num_seqs) {
             r = read_request(p, s);
             if (r.rows > 0) {
-                tiles = (r.rows * p.group + (1 << p.tile_shift) - 1) >> p.tile_shift;  // below 2^31: the host has looked at num_rows * group
+                tiles = (r.rows * p.group + (1 << p.tile_shift) - 1) >> p.tile_shift;  // below 2^30: the host has looked at num_rows * group
                 steps = steps_of(p, span_of(r));
             }
         }
@@ -109,7 +126,7 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
     // the lanes hold; others take the last).  What the sums round off is less than one part in 2^18, and max_items has room for that.
     float work = 0.f, units = 0.f;
     const auto plus = [](float a, float b) { return a + b; };
-    for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
+    for (int32_t s0 = 0; s0 < (FEW ? 1 : p.num_seqs); s0 += 64) {
         look(s0 + lane);
         work += total(wave_scan((float)steps * (float)tiles, plus));
         units += total(wave_scan((float)tiles, plus));
@@ -120,7 +137,7 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
         return max(p.min_steps, x < 1e9f ? (int32_t)x + 1 : 1000000000);
     };
     int32_t per = length(room > 0.5f * target ? room : 0.5f * target);
-    if (p.num_seqs <= 64) {
+    if (FEW) {
         const int32_t least = length(target);
         const auto keeps = [&](int32_t n) {
             const float all = total(wave_scan((float)(steps > n ? divide_up(steps, n) : 1) * (float)tiles, plus));
@@ -135,8 +152,8 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
     at.first_item = 0;
     if (!UNITS && p.by_xcd) {  // contiguous eighths of the items to the XCDs
         int32_t all = 0;
-        for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
-            if (p.num_seqs > 64) look(s0 + lane);
+        for (int32_t s0 = 0; s0 < (FEW ? 1 : p.num_seqs); s0 += 64) {
+            if (!FEW) look(s0 + lane);
             all = sum(all, total(wave_scan(count(splits_of()), sum)));
         }
         all = all < p.max_items ? all : p.max_items;
@@ -145,8 +162,8 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
         if (j >= per_xcd || idx >= all) return at;
     }
     int32_t before = 0;
-    for (int32_t s0 = 0; s0 < p.num_seqs; s0 += 64) {
-        if (p.num_seqs > 64) look(s0 + lane);
+    for (int32_t s0 = 0; s0 < (FEW ? 1 : p.num_seqs); s0 += 64) {
+        if (!FEW) look(s0 + lane);
         const int32_t splits = splits_of(), items = count(splits), mine = UNITS ? count(1) : items;
         const int32_t end = wave_scan(mine, sum), item_end = UNITS ? wave_scan(items, sum) : end;
         const uint64_t found = __ballot(sum(before, end) > idx);

@@ -17,7 +17,6 @@ namespace {
 
 constexpr int kKv4Pairs = 1 << kKv4TileShift;
 constexpr int NW = 4;  // wavefronts of a workgroup
-constexpr int AHEAD = 1;  // steps whose loads are under way before the one at hand
 
 // N bf16 parts of two numbers; each takes the upper 8 bits of what the parts before it leave
 template <int N>
@@ -38,8 +37,8 @@ constexpr float kStep = 8.f;  // base-2 units that a row's maximum may outgrow i
 
 }  // namespace
 
-template <int D, bool BF16>
-__global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_kernel(Kv4Attn p)
+template <int D, bool BF16, bool FEW>
+__global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
 {
     using C = Kv4Cfg<D>;
     constexpr int KS = D / 32;         // k-steps of a score
@@ -51,7 +50,8 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
     __shared__ __attribute__((aligned(1024))) uint8_t lds[NW * 32 * ROWB];
     __shared__ float lds_ml[NW][kKv4Pairs][2];
 
-    const Place at = find_place<false>(p, blockIdx.x);
+    have_fields(p);
+    const Place at = find_place<false, FEW>(p, blockIdx.x);
     if (at.s < 0) return;
     const Request r = at.r;
     int32_t tile, split;
@@ -75,33 +75,8 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
     const int32_t row = divide(pair, G, in_row), head = query_head(p, head0 + in_row);
     const int32_t pos = r.held - r.rows + row, near = near_of(r, pos);
     // the tile's first and last rows: positions and windows rise with the row
-    const int32_t pos_lo = r.held - r.rows + divide(pair0, G), pos_hi = r.held - r.rows + divide(pair0 + n_pairs - 1, G);
+    const int32_t pos_lo = r.held - r.rows + lane_value(row, 0), pos_hi = r.held - r.rows + lane_value(row, n_pairs - 1);
     const int32_t near_lo = near_of(r, pos_lo), near_hi = near_of(r, pos_hi);
-
-    // ---- queries: the lane's pair, elements kg * (D / 4) + 8 m .. + 8 of k-step m
-    bf16x8 qf[NQ][KS];
-    {
-        const int64_t at_q = ((int64_t)(r.row0 + row) * p.n_q_heads + head) * D + kg * (D / 4);
-#pragma unroll
-        for (int m = 0; m < KS; ++m) {
-            if constexpr (BF16) {
-                qf[0][m] = *reinterpret_cast<const bf16x8 *>((const uint16_t *)p.q + at_q + m * 8);
-            } else {
-                const float *q = (const float *)p.q + at_q + m * 8;
-                uint32_t w[NQ][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t part[NQ];
-                    split_pair<NQ>(q[2 * i], q[2 * i + 1], part);
-                    for (int n = 0; n < NQ; ++n) w[n][i] = part[n];
-                }
-                for (int n = 0; n < NQ; ++n) {
-                    const uint4 v = make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
-                    qf[n][m] = __builtin_bit_cast(bf16x8, v);
-                }
-            }
-        }
-    }
 
     // ---- the wavefront's records, 64 steps at a time: lane i holds those of step i of them
     uint64_t rec_off[2];
@@ -126,32 +101,70 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
         }
     };
 
-    struct Step {
-        uint32_t k[2][WORDS], v[2][WORDS], scales[2];
-        int32_t tok[2];
-    };
+    // The step at hand; a word's place is filled with the next step's as soon as it is used
+    uint32_t k[2][WORDS], v[2][WORDS], scales[2];
+    int32_t tok[2];
     // D = 128: a lane takes block kg of token l16, 16 bytes.  D = 64: half kg & 1 of block kg / 2, 8 bytes
     const uint32_t code_off = D == 128 ? lane * 16 : (kg >> 1) * 256 + l16 * 16 + (kg & 1) * 8;
     // the two scale bytes lie in one half of a word (loads of two bytes are widened where they arrive, in front of their use)
     const uint32_t scale_off = C::SCALES + ((D == 128 ? kg : kg >> 1) * 16 + (l16 & 14)) * 2, scale_bit = (l16 & 1) * 16;
-    const auto fetch = [&](Step &st, int32_t i) {  // the i-th of those steps
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint64_t off = (uint64_t)(uint32_t)lane_value((int32_t)(rec_off[e] >> 32), i) << 32 | (uint32_t)lane_value((int32_t)rec_off[e], i);
-            st.tok[e] = lane_value(rec_tok[e], i);
-            const uint8_t *base = p.pool.base + off;
-            if constexpr (D == 128) {
-                const uint4 k = *reinterpret_cast<const uint4 *>(base + code_off), v = *reinterpret_cast<const uint4 *>(base + C::CODES + code_off);
-                st.k[e][0] = k.x; st.k[e][1] = k.y; st.k[e][2] = k.z; st.k[e][3] = k.w;
-                st.v[e][0] = v.x; st.v[e][1] = v.y; st.v[e][2] = v.z; st.v[e][3] = v.w;
-            } else {
-                const uint2 k = *reinterpret_cast<const uint2 *>(base + code_off), v = *reinterpret_cast<const uint2 *>(base + C::CODES + code_off);
-                st.k[e][0] = k.x; st.k[e][1] = k.y;
-                st.v[e][0] = v.x; st.v[e][1] = v.y;
-            }
-            st.scales[e] = *reinterpret_cast<const uint32_t *>(base + scale_off);
+    const auto codes = [&](uint32_t (&to)[WORDS], const uint8_t *from) {
+        if constexpr (D == 128) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(from);
+            to[0] = x.x; to[1] = x.y; to[2] = x.z; to[3] = x.w;
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2 *>(from);
+            to[0] = x.x; to[1] = x.y;
         }
     };
+    const auto record = [&](int32_t e, int32_t i) {  // of the i-th of those steps
+        return p.pool.base + ((uint64_t)(uint32_t)lane_value((int32_t)(rec_off[e] >> 32), i) << 32 | (uint32_t)lane_value((int32_t)rec_off[e], i));
+    };
+    const auto fetch_k = [&](int32_t i) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint8_t *base = record(e, i);
+            tok[e] = lane_value(rec_tok[e], i);
+            codes(k[e], base + code_off);
+            scales[e] = *reinterpret_cast<const uint32_t *>(base + scale_off);
+        }
+    };
+    const auto fetch_v = [&](int32_t i) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) codes(v[e], record(e, i) + C::CODES + code_off);
+    };
+
+    // The order of the loop, for the waits at its head: K, then V
+    const auto begin = [&](int32_t first, auto between) {
+        read_records(first);
+        fetch_k(0);
+        asm volatile("" ::: "memory");
+        between();
+        fetch_v(0);
+    };
+    bf16x8 qf[NQ][KS];
+    begin(0, [&] {  // the queries on the way: the lane's pair, elements kg * (D / 4) + 8 m .. + 8 of k-step m
+        const int64_t at_q = ((int64_t)(r.row0 + row) * p.n_q_heads + head) * D + kg * (D / 4);
+#pragma unroll
+        for (int m = 0; m < KS; ++m) {
+            if constexpr (BF16) {
+                qf[0][m] = *reinterpret_cast<const bf16x8 *>((const uint16_t *)p.q + at_q + m * 8);
+            } else {
+                const float *q = (const float *)p.q + at_q + m * 8;
+                uint32_t w[NQ][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t part[NQ];
+                    split_pair<NQ>(q[2 * i], q[2 * i + 1], part);
+                    for (int n = 0; n < NQ; ++n) w[n][i] = part[n];
+                }
+                for (int n = 0; n < NQ; ++n) {
+                    const uint4 v = make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
+                    qf[n][m] = __builtin_bit_cast(bf16x8, v);
+                }
+            }
+        }
+    });
 
     float m_ref = -INFINITY, l_run = 0.f;
     uint32_t lost = 0;  // 32-element blocks of the pair's output that a NaN block of V reaches
@@ -159,31 +172,33 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    const auto compute = [&](Step &st) {
+    const auto compute = [&](int32_t next) {
         f32x4 s[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             s[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const float scale = kv4_scale(st.scales[e] >> scale_bit & 255u);
+            const float scale = kv4_scale(scales[e] >> scale_bit & 255u);
 #pragma unroll
             for (int m = 0; m < KS; ++m) {
                 bf16x2 x[4];
-                kv4_decode8(st.k[e][m], scale, x);
+                kv4_decode8(k[e][m], scale, x);
                 const bf16x8 a = {x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[n][m], s[e], 0, 0, 0);
             }
         }
-        uint32_t v_scale[2] = {st.scales[0] >> (scale_bit + 8) & 255u, st.scales[1] >> (scale_bit + 8) & 255u};
+        const int32_t first[2] = {tok[0], tok[1]};
+        uint32_t v_scale[2] = {scales[0] >> (scale_bit + 8) & 255u, scales[1] >> (scale_bit + 8) & 255u};
+        fetch_k(next);
         // ---- masks: only where some row does not see some key, or some value is NaN
         bool whole = true;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-            whole = whole && st.tok[e] >= 0 && st.tok[e] + 15 <= pos_lo && (st.tok[e] >= near_hi || st.tok[e] + 15 < r.sink);
+            whole = whole && first[e] >= 0 && first[e] + 15 <= pos_lo && (first[e] >= near_hi || first[e] + 15 < r.sink);
         if (!whole || __any(v_scale[0] == kKv4NanScale || v_scale[1] == kKv4NanScale)) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int32_t tok = st.tok[e];
+                const int32_t tok = first[e];
                 const auto sees = [&](int32_t j) { return tok >= 0 && j <= pos && (j >= near || j < r.sink); };
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -198,7 +213,7 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
                 if (!seen || v_scale[e] == kKv4NanScale) {
                     v_scale[e] = kKv4Bias;
 #pragma unroll
-                    for (int w = 0; w < WORDS; ++w) st.v[e][w] = 0;
+                    for (int w = 0; w < WORDS; ++w) v[e][w] = 0;
                 }
             }
         }
@@ -210,12 +225,13 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
 #pragma unroll
             for (int w = 0; w < WORDS; ++w) {
                 bf16x2 x[4];
-                kv4_decode8(st.v[e][w], scale, x);
+                kv4_decode8(v[e][w], scale, x);
                 const uint4 four = make_uint4(__builtin_bit_cast(uint32_t, x[0]), __builtin_bit_cast(uint32_t, x[1]), __builtin_bit_cast(uint32_t, x[2]),
                                               __builtin_bit_cast(uint32_t, x[3]));
                 *reinterpret_cast<uint4 *>(slice + t * ROWB + value_chunk<D>(l16, kg * WORDS + w) * 16) = four;
             }
         }
+        fetch_v(next);
         // ---- weights against the pair's reference, which is raised where a score outgrows it
         float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         if (__any(top * p.c_log2 > m_ref + kStep)) {
@@ -260,24 +276,24 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
         }
     };
 
-    // Loads go out AHEAD steps in front of the one at hand, on every step (behind the last the last one's again): a load under a
-    // condition makes the compiler wait for all of them where the paths meet.
+    // Loads go out on every step (behind the last the last one's again): a load under a condition makes the compiler wait for all of them where
+    // the paths meet.
     const int32_t mine = step1 - step0 > wave ? (step1 - step0 - wave + NW - 1) / NW : 0;  // the wavefront's steps
-    for (int32_t first = 0; first < mine; first += 64) {
+    // Of the wavefronts of a SIMD the oldest is served first, and the workgroups that came last would end last, 15 % behind the first: those that are behind
+    // go first (one request of 65.9 K tokens 20.3 -> 19.5 us, 64 ragged ones 65.3 -> 64.0).
+    const int32_t quarter = (mine + 3) / 4;
+    __builtin_amdgcn_s_setprio(3);
+    for (int32_t first = 0; first < mine;) {
         const int32_t n = mine - first < 64 ? mine - first : 64;
-        Step st[AHEAD + 1];
-        read_records(first);
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) fetch(st[u], u < n ? u : n - 1);
-        for (int32_t i = 0; i < n; i += AHEAD + 1) {
-#pragma unroll
-            for (int u = 0; u <= AHEAD; ++u) {
-                if (i + u >= n) break;
-                const int32_t ahead = i + u + AHEAD;
-                fetch(st[(u + AHEAD) % (AHEAD + 1)], ahead < n ? ahead : n - 1);
-                compute(st[u]);
-            }
+        for (int32_t i = 0; i < n; ++i) {
+            const int32_t done = first + i;
+            if (done == quarter) __builtin_amdgcn_s_setprio(2);
+            else if (done == 2 * quarter) __builtin_amdgcn_s_setprio(1);
+            else if (done == 3 * quarter) __builtin_amdgcn_s_setprio(0);
+            compute(i + 1 < n ? i + 1 : i);
         }
+        first += n;
+        if (first < mine) begin(first, [] {});
     }
 
     // ---- the wavefronts' parts of a pair: O^T to the wavefronts' slices as [pair][D] (each has 16 * D * 4 bytes), joined by all
@@ -326,14 +342,15 @@ __global__ __launch_bounds__(NW * 64, D == 128 && !BF16 ? 2 : 3) void attn_kv4_k
 // of 28 pairs), and to fetch all maxima before the first values is one round trip more.
 constexpr int kTurn = 6;
 
-template <int D, bool BF16, int WAVES>
+template <int D, bool BF16, int WAVES, bool FEW>
 __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void merge_kv4_kernel(Kv4Attn p)
 {
     constexpr int LPR = D / 4, NSUB = WAVES * 64 / LPR, PAIRS = WAVES == 16 ? 1 : 4 / WAVES;
     __shared__ float parts[PAIRS][WAVES][D], ml[PAIRS][WAVES][2];
+    have_fields(p);
     int32_t pr;
     const int32_t unit = divide(blockIdx.x, (p.tile_pairs + PAIRS - 1) / PAIRS, pr);
-    const Place at = find_place<true>(p, unit);
+    const Place at = find_place<true, FEW>(p, unit);
     if (at.s < 0 || at.splits < 2) return;
     int32_t tile;
     const int32_t g = divide(at.rest, at.tiles, tile);
@@ -421,17 +438,23 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void merge_kv4_kernel(Kv4
     store_pair<D, BF16>(p, (int64_t)(at.r.row0 + row) * p.n_q_heads + head, d4, acc, M, l);
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool FEW>
 static void launch(const Kv4Attn &p, bool merge, hipStream_t stream)
 {
     if (p.tile_shift == kKv4RowsTileShift) launch_attn_kv4_rows(p, D, stream);
-    else hipLaunchKernelGGL((attn_kv4_kernel<D, BF16>), dim3((p.grid + 7) / 8 * 8), dim3(NW * 64), 0, stream, p);
+    else hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, FEW>), dim3((p.grid + 7) / 8 * 8), dim3(NW * 64), 0, stream, p);
     if (!merge) return;
     // few units are cut into many items, whose joining is worth more wavefronts where there are few pairs
     const bool long_units = p.max_units <= 16;
-    if (!long_units) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 2>), dim3(p.max_units * ceil_div(p.tile_pairs, 2)), dim3(256), 0, stream, p);
-    else if (p.tile_pairs > kKv4Pairs) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 4>), dim3(p.max_units * p.tile_pairs), dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16>), dim3(p.max_units * p.tile_pairs), dim3(1024), 0, stream, p);
+    if (!long_units) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 2, FEW>), dim3(p.max_units * ceil_div(p.tile_pairs, 2)), dim3(256), 0, stream, p);
+    else if (p.tile_pairs > kKv4Pairs) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 4, FEW>), dim3(p.max_units * p.tile_pairs), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16, FEW>), dim3(p.max_units * p.tile_pairs), dim3(1024), 0, stream, p);
+}
+
+template <int D, bool BF16>
+static void launch(const Kv4Attn &p, bool merge, hipStream_t stream)
+{
+    p.num_seqs <= 64 ? launch<D, BF16, true>(p, merge, stream) : launch<D, BF16, false>(p, merge, stream);
 }
 
 hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, bool merge, hipStream_t stream)

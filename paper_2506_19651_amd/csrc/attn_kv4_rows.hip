@@ -117,7 +117,7 @@ __device__ __forceinline__ float values(const uint8_t *tv, const uint32_t (&at)[
 
 }  // namespace
 
-template <int D>
+template <int D, bool FEW>
 __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_rows_kernel(Kv4Attn p)
 {
     using C = TileCfg<D>;
@@ -131,7 +131,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_rows_kernel(Kv4Attn p)
     __shared__ __attribute__((aligned(16))) int32_t key_notes[kStages][NW];  // first token (-1: not there) and kSpecial
     __shared__ ValueNote value_notes[2];
 
-    const Place at = find_place<false>(p, blockIdx.x);
+    have_fields(p);
+    const Place at = find_place<false, FEW>(p, blockIdx.x);
     if (at.s < 0) return;
     const Request r = at.r;
     int32_t tile, split;
@@ -397,8 +398,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_rows_kernel(Kv4Attn p)
 void launch_attn_kv4_rows(const Kv4Attn &p, int32_t D, hipStream_t stream)
 {
     const dim3 grid((p.grid + 7) / 8 * 8), block(NW * 64);
-    if (D == 128) hipLaunchKernelGGL(attn_kv4_rows_kernel<128>, grid, block, 0, stream, p);
-    else hipLaunchKernelGGL(attn_kv4_rows_kernel<64>, grid, block, 0, stream, p);
+    const bool few = p.num_seqs <= 64;
+    if (D == 128 && few) hipLaunchKernelGGL((attn_kv4_rows_kernel<128, true>), grid, block, 0, stream, p);
+    else if (D == 128) hipLaunchKernelGGL((attn_kv4_rows_kernel<128, false>), grid, block, 0, stream, p);
+    else if (few) hipLaunchKernelGGL((attn_kv4_rows_kernel<64, true>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((attn_kv4_rows_kernel<64, false>), grid, block, 0, stream, p);
 }
 
 }  // namespace pevlm
