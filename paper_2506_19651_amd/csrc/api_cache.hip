@@ -113,7 +113,7 @@ static void size_attn(const pevlm_heads *h, int32_t num_seqs, int32_t num_rows, 
     const int32_t resident = many ? 2 : (h->head_dim == 64 ? 4 : 3);
     p->target = resident * compute_units();
     p->min_steps = many ? 4 : 12;
-    p->by_xcd = pairs > asking << p->tile_shift;
+    p->shared = pairs > asking << p->tile_shift;
     const int64_t units = h->n_kv_heads * (asking + (pairs >> p->tile_shift));
     p->max_units = (int32_t)std::min<int64_t>(units, INT32_MAX);
     p->max_items = (int32_t)std::min<int64_t>(units + p->target + 8, INT32_MAX);

@@ -87,18 +87,19 @@ __device__ __forceinline__ void have_fields(const Kv4Attn &p)
 {
     asm volatile("" ::"s"(p.q), "s"(p.out), "s"(p.lse), "s"(p.pool.base), "s"(p.pool.num_pages), "s"(p.pool.page_shift), "s"(p.pool.n_kv_heads), "s"(p.table),
                  "s"(p.row_start), "s"(p.row_len), "s"(p.seq_len), "s"(p.sink_len), "s"(p.window), "s"(p.part_acc), "s"(p.part_ml), "s"(p.num_seqs),
-                 "s"(p.max_pages), "s"(p.num_rows), "s"(p.n_q_heads), "s"(p.tile_pairs), "s"(p.group), "s"(p.mapped), "s"(p.by_xcd), "s"(p.target),
+                 "s"(p.max_pages), "s"(p.num_rows), "s"(p.n_q_heads), "s"(p.tile_pairs), "s"(p.group), "s"(p.mapped), "s"(p.target),
                  "s"(p.min_steps), "s"(p.max_items), "s"(p.c_log2));
 }
 
 // Where the idx-th item (or unit) of a call lies.  Every wavefront finds its own by itself: lane by lane over 64 requests at a
-// time, once for the whole work, which sets the items' length, and once for the place.  FEW: up to 64 requests, which the lanes keep.
+// time, once for the whole work, which sets the items' length, and once for the place.  FEW: up to 64 requests, which the lanes keep; SHARED:
+// contiguous eighths of the items go to the XCDs, as tiles of the same keys are neighbours.
 struct Place {
     int32_t s, first_item, splits, tiles, rest;  // rest: the item's (unit's) place within the request
     Request r;
 };
 
-template <bool UNITS, bool FEW>
+template <bool UNITS, bool FEW, bool SHARED = false>
 __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
 {
     const int32_t lane = threadIdx.x & 63;
@@ -150,7 +151,7 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
     Place at;
     at.s = -1;
     at.first_item = 0;
-    if (!UNITS && p.by_xcd) {  // contiguous eighths of the items to the XCDs
+    if (SHARED) {
         int32_t all = 0;
         for (int32_t s0 = 0; s0 < (FEW ? 1 : p.num_seqs); s0 += 64) {
             if (!FEW) look(s0 + lane);

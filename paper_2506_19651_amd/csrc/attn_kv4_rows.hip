@@ -132,7 +132,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_rows_kernel(Kv4Attn p)
     __shared__ ValueNote value_notes[2];
 
     have_fields(p);
-    const Place at = find_place<false, FEW>(p, blockIdx.x);
+    const Place at = find_place<false, FEW, true>(p, blockIdx.x);
     if (at.s < 0) return;
     const Request r = at.r;
     int32_t tile, split;

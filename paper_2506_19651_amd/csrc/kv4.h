@@ -82,7 +82,7 @@ struct Kv4Attn {
     int32_t tile_pairs;               // pairs that a tile can have: all of a tile, or all that the rows make
     int32_t group;                    // query heads of the KV head that has most
     int32_t mapped;                   // whether a head map is given
-    int32_t by_xcd;                   // whether an XCD takes neighbouring items, as tiles of the same keys are
+    int32_t shared;                   // whether there may be several tiles of the same keys
     int32_t target, min_steps;        // items that a call is cut into, if they are not shorter than this
     int32_t max_items, max_units;     // bounds that no lengths pass
     int32_t grid;                     // and one for the items that the table's width allows
