@@ -83,36 +83,48 @@ static int32_t group_heads(const HeadTable &tab, const pevlm_heads *h, Kv4Heads 
     return most;
 }
 
-// Whether the kernel of many rows is taken: by the tiles of 16 and of 128 that a request's (row, query head) pairs of a KV head fill, on average.  A
-// tile of 128 takes the time of four of 16, of 64-wide heads of seven.  One request of 65.9 K tokens, 16 / 128: 28/4 heads x 128, 7 rows 33.8 / 34.6 us,
-// 14 rows 47.1 / 41.0, 20 rows 55.1 / 55.7, 40 rows 96 / 72, 128 rows 282 / 145; 32/8 heads 14 rows 49.6 / 50.4, 28 rows 78 / 59; 14/2 heads x 64, 18
-// rows 26.8 / 28.5, 128 rows 92 / 66.  Up to a few thousand tokens its start and longer steps do not pay (2000 tokens x 28/4, 14 rows 14.8 / 17.9, 60
-// rows 21.0 / 24.4, 128 rows 28.3 / 28.1): how long a request is stands on the GPU, the table's width is looked at.
-constexpr int64_t kManyRowsTokens = 4096;
-static bool many_rows(const pevlm_heads *h, int32_t group, int32_t num_seqs, int32_t num_rows, int64_t width)
+// How a call is cut.  A request with r rows has ceil(r * group / tile) tiles of (row, query head) pairs of a KV head; tiles are of 16 pairs, of 32 in the
+// same kernel, or of 128 in the kernel of many rows.  How long a request is stands on the GPU: the table's width is looked at.
+enum class Cut { kTiles16, kTiles32, kTiles128 };
+
+static int32_t asking_of(int32_t num_seqs, int32_t num_rows) { return std::max(1, std::min(num_seqs, num_rows)); }
+
+// Workgroups of 16 pairs that a compute unit holds at a time, by registers
+static int32_t resident16(const pevlm_heads *h) { return h->head_dim == 64 ? 4 : 3; }
+
+// Tiles of 128: by the tiles of 16 and of 128 that a request's pairs fill, on average.  A tile of 128 takes the time of four of 16, of 64-wide heads of
+// seven.  One request of 65.9 K tokens, 16 / 128: 28/4 heads x 128, 7 rows 33.8 / 34.6 us, 14 rows 47.1 / 41.0, 20 rows 55.1 / 55.7, 40 rows 96 / 72, 128
+// rows 282 / 145; 32/8 heads 14 rows 49.6 / 50.4, 28 rows 78 / 59; 14/2 heads x 64, 18 rows 26.8 / 28.5, 128 rows 92 / 66.  Up to a few thousand
+// tokens its start and longer steps do not pay (2000 tokens x 28/4, 14 rows 14.8 / 17.9, 60 rows 21.0 / 24.4, 128 rows 28.3 / 28.1).
+//
+// Tiles of 32 decode a record for two tiles of 16, and a unit has half as many workgroups: they pay by the steps that a workgroup of 16 would have.
+// 16 / 32: 64 requests of 16 K tokens x 28/4, 4 rows (333 steps) 190 / 153 us; 16 of 65.9 K x 14/2 x 64, 4 rows (129) 62 / 53; fp32 32 rows of one of
+// 65.9 K (150) 96 / 88; fp32 16 of 16 K, 4 rows (83) 65 / 64; 8 rows of one (43) 32.5 / 32.0; 4 rows of one (21) 25.0 / 26.7; 64 of 1000, 3
+// rows (21) 25.8 / 32.3.
+constexpr int64_t kManyRowsTokens = 4096, kTiles32Steps = 64;
+static Cut cut_of(const pevlm_heads *h, int32_t group, int32_t num_seqs, int32_t num_rows, int64_t width)
 {
-    if (h->dtype != PEVLM_BF16 || width < kManyRowsTokens) return false;
-    const int64_t asking = std::max(1, std::min(num_seqs, num_rows)), pairs = ((int64_t)num_rows * group + asking - 1) / asking;
-    return (pairs + 15) / 16 > (h->head_dim == 128 ? 4 : 7) * ((pairs + 127) / 128);
+    const int64_t asking = asking_of(num_seqs, num_rows), pairs = ((int64_t)num_rows * group + asking - 1) / asking;
+    const int64_t tiles16 = (pairs + 15) / 16, tiles128 = (pairs + 127) / 128;
+    if (h->dtype == PEVLM_BF16 && width >= kManyRowsTokens && tiles16 > (h->head_dim == 128 ? 4 : 7) * tiles128) return Cut::kTiles128;
+    const double steps = (double)asking * tiles16 * h->n_kv_heads * (double)(width >> (4 + kKv4StepShift)) / (resident16(h) * compute_units());
+    return tiles16 > 1 && steps >= kTiles32Steps ? Cut::kTiles32 : Cut::kTiles16;
 }
 
-// What bounds a call's items, and how it is cut.  A request with r rows has ceil(r * group / tile) tiles of a KV head.
-static void size_attn(const pevlm_heads *h, int32_t num_seqs, int32_t num_rows, int64_t width, Kv4Attn *p)
+// What bounds a call's items
+static void size_attn(const pevlm_heads *h, const HeadTable &tab, int32_t num_seqs, int32_t num_rows, Cut cut, Kv4Attn *p)
 {
-    HeadTable tab;
-    check_heads(h, &tab);
     p->group = group_heads(tab, h, &p->heads);
     p->mapped = h->kv_head_of_q != nullptr;
-    const int64_t asking = std::max(1, std::min(num_seqs, num_rows)), pairs = (int64_t)num_rows * p->group;
-    const bool many = many_rows(h, p->group, num_seqs, num_rows, width);
-    p->tile_shift = many ? kKv4RowsTileShift : kKv4TileShift;
+    const int64_t asking = asking_of(num_seqs, num_rows), pairs = (int64_t)num_rows * p->group;
+    const bool many = cut == Cut::kTiles128;
+    p->tile_shift = many ? kKv4RowsTileShift : (cut == Cut::kTiles32 ? kKv4TileShift + 1 : kKv4TileShift);
     p->step_shift = many ? kKv4RowsStepShift : kKv4StepShift;
     p->tile_pairs = (int32_t)std::min<int64_t>(1 << p->tile_shift, pairs);
-    // workgroups that a compute unit holds at a time: a call is one round of them.  (Two rounds of shorter items are 3 % slower, 16 requests of
-    // 65.9 K tokens 116.5 -> 119.4 us, four 8 %: an item's start and end, some 6 us, come twice.)
-    const int32_t resident = many ? 2 : (h->head_dim == 64 ? 4 : 3);
-    p->target = resident * compute_units();
-    p->min_steps = many ? 4 : 12;
+    // A call is one round of the workgroups that the compute units hold: a tile of 32 takes the registers of one more.  (Two rounds of shorter items are
+    // 3 % slower, 16 requests of 65.9 K tokens 116.5 -> 119.4 us, four 8 %: an item's start and end, some 6 us, come twice.)
+    p->target = (many ? 2 : resident16(h) - (cut == Cut::kTiles32 ? 1 : 0)) * compute_units();
+    p->min_steps = many ? 4 : 8;  // 8 / 12: one request of 8000 tokens 12.5 / 13.1 us, of 30 K 15.8 / 16.7
     p->shared = pairs > asking << p->tile_shift;
     const int64_t units = h->n_kv_heads * (asking + (pairs >> p->tile_shift));
     p->max_units = (int32_t)std::min<int64_t>(units, INT32_MAX);
@@ -208,10 +220,13 @@ size_t pevlm_cache_attn_workspace_bytes(const pevlm_heads *heads, int32_t num_se
         fail(PEVLM_ERR_INVALID_ARG, "need num_seqs >= 1 and num_rows >= 0");
         return 0;
     }
+    HeadTable tab;
+    check_heads(heads, &tab);
     Kv4Attn p;
     size_t bytes = 0;
-    for (int64_t width : {(int64_t)0, kManyRowsTokens}) {  // a call is cut one way or the other by its table
-        size_attn(heads, num_seqs, num_rows, width, &p);
+    // A call's cut depends on its table's width: tiles of 16 up to one, of 32 from there on, or of 128 from kManyRowsTokens on
+    for (int64_t width : {(int64_t)0, kManyRowsTokens - 1, (int64_t)kMaxTokens}) {
+        size_attn(heads, tab, num_seqs, num_rows, cut_of(heads, group_heads(tab, heads, &p.heads), num_seqs, num_rows, width), &p);
         bytes = std::max(bytes, attn_bytes(p, heads->head_dim));
     }
     return bytes + 256;
@@ -223,7 +238,8 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
 {
     Kv4Attn p;
     memset(&p, 0, sizeof p);
-    pevlm_status st = check_heads(heads, nullptr);
+    HeadTable tab;
+    pevlm_status st = check_heads(heads, &tab);
     if (st == PEVLM_OK) st = check_pool(cache, &p.pool, heads->n_kv_heads);
     if (st == PEVLM_OK) st = check_table(cache);
     if (st == PEVLM_OK) st = check_pool_memory(cache);
@@ -234,7 +250,8 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
     if (!row_start || !row_len || !seq_len) return fail(PEVLM_ERR_INVALID_ARG, "row_start, row_len and seq_len must not be NULL");
     for (const int32_t *a : {row_start, row_len, seq_len, sink_len, window, (const int32_t *)lse})
         if (!aligned4(a)) return fail(PEVLM_ERR_INVALID_ARG, "arrays must be 4-byte aligned");
-    size_attn(heads, cache->num_seqs, num_rows, (int64_t)cache->max_pages * cache->page_size, &p);
+    const int64_t width = (int64_t)cache->max_pages * cache->page_size;
+    size_attn(heads, tab, cache->num_seqs, num_rows, cut_of(heads, group_heads(tab, heads, &p.heads), cache->num_seqs, num_rows, width), &p);
     if (p.max_items > 0x3fffffff || ((int64_t)p.max_units << p.tile_shift) > 1 << 30) return fail(PEVLM_ERR_UNSUPPORTED, "too many work items");
     const size_t need = attn_bytes(p, heads->head_dim);
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))
@@ -249,7 +266,7 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
     p.n_q_heads = heads->n_q_heads;
     p.part_ml = (float *)workspace;
     // no request is longer than its row of the table
-    const int64_t longest = ceil_div(ceil_div(cache->max_pages * cache->page_size, kKv4Record << p.step_shift), p.min_steps);
+    const int64_t longest = ceil_div((int32_t)((width + (kKv4Record << p.step_shift) - 1) / (kKv4Record << p.step_shift)), p.min_steps);
     p.grid = (int32_t)std::min<int64_t>(p.max_items, p.max_units * longest);
     p.part_acc = (float *)((char *)workspace + ml_bytes(p));
     p.c_log2 = scale_of(heads) * 1.4426950408889634f;

@@ -15,7 +15,6 @@ namespace pevlm {
 
 namespace {
 
-constexpr int kKv4Pairs = 1 << kKv4TileShift;
 constexpr int NW = 4;  // wavefronts of a workgroup
 
 // N bf16 parts of two numbers; each takes the upper 8 bits of what the parts before it leave
@@ -49,8 +48,9 @@ constexpr float kStep = 8.f;  // base-2 units that a row's maximum may outgrow i
 
 }  // namespace
 
-template <int D, bool BF16, bool FEW, bool SHARED>
-__global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
+// PT: tiles of 16 pairs that share the decoded records; SHARED: whether other workgroups read the same codes
+template <int D, bool BF16, int PT, bool SHARED, bool FEW>
+__global__ __launch_bounds__(NW * 64, PT == 1 ? 3 : 2) void attn_kv4_kernel(Kv4Attn p)
 {
     using C = Kv4Cfg<D>;
     constexpr int KS = D / 32;         // k-steps of a score
@@ -60,7 +60,8 @@ __global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
     constexpr int WORDS = D / 32;      // words of codes of a lane: 32 (16) elements of D = 128 (64)
     static_assert(WORDS == KS, "a lane's word is its share of a k-step");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[NW * 32 * ROWB];
-    __shared__ float lds_ml[NW][kKv4Pairs][2];
+    constexpr int PAIRS = 16 * PT;
+    __shared__ float lds_ml[NW][PAIRS][2];
 
     have_fields(p);
     const Place at = find_place<false, FEW, SHARED>(p, blockIdx.x);
@@ -70,8 +71,8 @@ __global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
     const int32_t g = divide(divide(at.rest, at.tiles, tile), at.splits, split);
     const int32_t item = at.first_item + at.rest;
     const int32_t head0 = first_head(p, g), G = heads_of(p, g);
-    const int32_t pair0 = tile * kKv4Pairs, n_pairs_all = r.rows * G;
-    const int32_t n_pairs = n_pairs_all - pair0 < kKv4Pairs ? n_pairs_all - pair0 : kKv4Pairs;
+    const int32_t pair0 = tile * PAIRS, n_pairs_all = r.rows * G;
+    const int32_t n_pairs = n_pairs_all - pair0 < PAIRS ? n_pairs_all - pair0 : PAIRS;
     if (n_pairs <= 0) return;
     const Span span = span_of(r);
     const int32_t steps = steps_of(p, span), per = divide_up(steps, at.splits);
@@ -81,13 +82,18 @@ __global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
     const int32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     uint8_t *const slice = lds + wave * 32 * ROWB;
 
-    // this lane's pair (column of S^T)
-    const int32_t pair = pair0 + (l16 < n_pairs ? l16 : n_pairs - 1);
-    int32_t in_row;
-    const int32_t row = divide(pair, G, in_row), head = query_head(p, head0 + in_row);
-    const int32_t pos = r.held - r.rows + row, near = near_of(r, pos);
+    // this lane's pairs (columns of S^T)
+    int32_t row[PT], head[PT], pos[PT], near[PT];
+#pragma unroll
+    for (int u = 0; u < PT; ++u) {
+        int32_t in_row;
+        row[u] = divide(pair0 + min(u * 16 + l16, n_pairs - 1), G, in_row);
+        head[u] = query_head(p, head0 + in_row);
+        pos[u] = r.held - r.rows + row[u];
+        near[u] = near_of(r, pos[u]);
+    }
     // the tile's first and last rows: positions and windows rise with the row
-    const int32_t pos_lo = r.held - r.rows + lane_value(row, 0), pos_hi = r.held - r.rows + lane_value(row, n_pairs - 1);
+    const int32_t pos_lo = lane_value(pos[0], 0), pos_hi = lane_value(pos[PT - 1], 15);
     const int32_t near_lo = near_of(r, pos_lo), near_hi = near_of(r, pos_hi);
 
     // ---- the wavefront's records, 64 steps at a time: lane i holds those of step i of them
@@ -154,41 +160,51 @@ __global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
         between();
         fetch_v(0);
     };
-    bf16x8 qf[NQ][KS];
+    bf16x8 qf[PT][NQ][KS];
     begin(0, [&] {  // the queries on the way: the lane's pair, elements kg * (D / 4) + 8 m .. + 8 of k-step m
-        const int64_t at_q = ((int64_t)(r.row0 + row) * p.n_q_heads + head) * D + kg * (D / 4);
 #pragma unroll
-        for (int m = 0; m < KS; ++m) {
-            if constexpr (BF16) {
-                qf[0][m] = *reinterpret_cast<const bf16x8 *>((const uint16_t *)p.q + at_q + m * 8);
-            } else {
-                const float *q = (const float *)p.q + at_q + m * 8;
-                uint32_t w[NQ][4];
+        for (int u = 0; u < PT; ++u) {
+            const int64_t at_q = ((int64_t)(r.row0 + row[u]) * p.n_q_heads + head[u]) * D + kg * (D / 4);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t part[NQ];
-                    split_pair<NQ>(q[2 * i], q[2 * i + 1], part);
-                    for (int n = 0; n < NQ; ++n) w[n][i] = part[n];
-                }
-                for (int n = 0; n < NQ; ++n) {
-                    const uint4 v = make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
-                    qf[n][m] = __builtin_bit_cast(bf16x8, v);
+            for (int m = 0; m < KS; ++m) {
+                if constexpr (BF16) {
+                    qf[u][0][m] = *reinterpret_cast<const bf16x8 *>((const uint16_t *)p.q + at_q + m * 8);
+                } else {
+                    const float *q = (const float *)p.q + at_q + m * 8;
+                    uint32_t w[NQ][4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t part[NQ];
+                        split_pair<NQ>(q[2 * i], q[2 * i + 1], part);
+                        for (int n = 0; n < NQ; ++n) w[n][i] = part[n];
+                    }
+                    for (int n = 0; n < NQ; ++n) {
+                        const uint4 v = make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
+                        qf[u][n][m] = __builtin_bit_cast(bf16x8, v);
+                    }
                 }
             }
         }
     });
 
-    float m_ref = -INFINITY, l_run = 0.f;
-    uint32_t lost = 0;  // 32-element blocks of the pair's output that a NaN block of V reaches
-    f32x4 o[DT];
+    float m_ref[PT], l_run[PT];
+    uint32_t lost[PT];  // 32-element blocks of the pair's output that a NaN block of V reaches
+    f32x4 o[PT][DT];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < PT; ++u) {
+        m_ref[u] = -INFINITY;
+        l_run[u] = 0.f;
+        lost[u] = 0;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
 
     const auto compute = [&](int32_t next) {
-        f32x4 s[2];
+        f32x4 s[PT][2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            s[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < PT; ++u) s[u][e] = f32x4{0.f, 0.f, 0.f, 0.f};
             const float scale = kv4_scale(scales[e] >> scale_bit & 255u);
 #pragma unroll
             for (int m = 0; m < KS; ++m) {
@@ -196,7 +212,9 @@ __global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
                 kv4_decode8(k[e][m], scale, x);
                 const bf16x8 a = {x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) s[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[n][m], s[e], 0, 0, 0);
+                for (int u = 0; u < PT; ++u)
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) s[u][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[u][n][m], s[u][e], 0, 0, 0);
             }
         }
         const int32_t first[2] = {tok[0], tok[1]};
@@ -211,16 +229,20 @@ __global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int32_t tok = first[e];
-                const auto sees = [&](int32_t j) { return tok >= 0 && j <= pos && (j >= near || j < r.sink); };
+                const auto sees = [&](int u, int32_t j) { return tok >= 0 && j <= pos[u] && (j >= near[u] || j < r.sink); };
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (!sees(tok + kg * 4 + i)) s[e][i] = -INFINITY;
+                for (int u = 0; u < PT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!sees(u, tok + kg * 4 + i)) s[u][e][i] = -INFINITY;
                 // the values of a key that no row sees, and NaN blocks, count as 0
                 const int32_t mine = tok + l16;
                 const bool seen = tok >= 0 && mine <= pos_hi && (mine >= near_lo || mine < r.sink);
                 for (uint64_t bad = __ballot(seen && v_scale[e] == kKv4NanScale); bad; bad &= bad - 1) {
                     const int32_t from = __builtin_ctzll(bad);
-                    if (sees(tok + (from & 15))) lost |= 1u << (D == 128 ? from >> 4 : from >> 5);
+#pragma unroll
+                    for (int u = 0; u < PT; ++u)
+                        if (sees(u, tok + (from & 15))) lost[u] |= 1u << (D == 128 ? from >> 4 : from >> 5);
                 }
                 if (!seen || v_scale[e] == kKv4NanScale) {
                     v_scale[e] = kKv4Bias;
@@ -245,29 +267,34 @@ __global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
         }
         fetch_v(next);
         // ---- weights against the pair's reference, which is raised where a score outgrows it
-        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        if (__any(top * p.c_log2 > m_ref + kStep)) {
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32)) * p.c_log2;
-            if (top > m_ref + kStep) {
-                const float alpha = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - top);
-                m_ref = top;
-                l_run *= alpha;
+        uint32_t pw[PT][NP][4];
 #pragma unroll
-                for (int t = 0; t < DT; ++t) o[t] *= alpha;
+        for (int u = 0; u < PT; ++u) {
+            const f32x4 a = s[u][0], b = s[u][1];
+            float top = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3])));
+            if (__any(top * p.c_log2 > m_ref[u] + kStep)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32)) * p.c_log2;
+                if (top > m_ref[u] + kStep) {
+                    const float alpha = m_ref[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[u] - top);
+                    m_ref[u] = top;
+                    l_run[u] *= alpha;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) o[u][t] *= alpha;
+                }
             }
-        }
-        const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-        uint32_t pw[NP][4];
+            const float ref = m_ref[u] == -INFINITY ? 0.f : m_ref[u];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = i >> 1, j = (i & 1) * 2;
-            const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e][j], p.c_log2, -ref)), b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e][j + 1], p.c_log2, -ref));
-            l_run += a + b;
-            uint32_t part[NP];
-            split_pair<NP>(a, b, part);
+            for (int i = 0; i < 4; ++i) {
+                const int e = i >> 1, j = (i & 1) * 2;
+                const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e][j], p.c_log2, -ref));
+                const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e][j + 1], p.c_log2, -ref));
+                l_run[u] += w0 + w1;
+                uint32_t part[NP];
+                split_pair<NP>(w0, w1, part);
 #pragma unroll
-            for (int n = 0; n < NP; ++n) pw[n][i] = part[n];
+                for (int n = 0; n < NP; ++n) pw[u][n][i] = part[n];
+            }
         }
         // ---- O^T += V^T P^T: k index kg * 8 + j is token kg * 4 + j of the first record, j < 4, or + j - 4 of the second
 #pragma unroll
@@ -281,10 +308,12 @@ __global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
                 a[e * 4] = four[0]; a[e * 4 + 1] = four[1]; a[e * 4 + 2] = four[2]; a[e * 4 + 3] = four[3];
             }
 #pragma unroll
-            for (int n = 0; n < NP; ++n) {
-                const uint4 b = make_uint4(pw[n][0], pw[n][1], pw[n][2], pw[n][3]);
-                o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, b), o[t], 0, 0, 0);
-            }
+            for (int u = 0; u < PT; ++u)
+#pragma unroll
+                for (int n = 0; n < NP; ++n) {
+                    const uint4 b = make_uint4(pw[u][n][0], pw[u][n][1], pw[u][n][2], pw[u][n][3]);
+                    o[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, b), o[u][t], 0, 0, 0);
+                }
         }
     };
 
@@ -309,41 +338,46 @@ __global__ __launch_bounds__(NW * 64, 3) void attn_kv4_kernel(Kv4Attn p)
     }
 
     // ---- the wavefronts' parts of a pair: O^T to the wavefronts' slices as [pair][D] (each has 16 * D * 4 bytes), joined by all
-    l_run += __shfl_xor(l_run, 16);
-    l_run += __shfl_xor(l_run, 32);
     float *const mine_o = reinterpret_cast<float *>(slice);
-#pragma unroll
-    for (int t = 0; t < DT; ++t) {
-        if (lost >> (t >> 1) & 1u) o[t] = f32x4{NAN, NAN, NAN, NAN};
-        *reinterpret_cast<f32x4 *>(mine_o + l16 * D + t * 16 + kg * 4) = o[t];
-    }
-    if (kg == 0) {
-        lds_ml[wave][l16][0] = m_ref;
-        lds_ml[wave][l16][1] = l_run;
-    }
-    __syncthreads();
     const float *const all_o = reinterpret_cast<const float *>(lds);
-    for (int32_t i = tid; i < n_pairs * (D / 4); i += NW * 64) {
-        const int32_t pr = i / (D / 4), d4 = i % (D / 4) * 4;
-        float M = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) M = fmaxf(M, lds_ml[w][pr][0]);
-        const float ref = M == -INFINITY ? 0.f : M;
-        float l = 0.f;
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < PT; ++u) {
+        if (u > 0) __syncthreads();
+        l_run[u] += __shfl_xor(l_run[u], 16);
+        l_run[u] += __shfl_xor(l_run[u], 32);
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float f = __builtin_amdgcn_exp2f(lds_ml[w][pr][0] - ref);
-            l += f * lds_ml[w][pr][1];
-            acc += f * *reinterpret_cast<const f32x4 *>(all_o + (w * kKv4Pairs + pr) * D + d4);
+        for (int t = 0; t < DT; ++t) {
+            if (lost[u] >> (t >> 1) & 1u) o[u][t] = f32x4{NAN, NAN, NAN, NAN};
+            *reinterpret_cast<f32x4 *>(mine_o + l16 * D + t * 16 + kg * 4) = o[u][t];
         }
-        if (at.splits > 1) {
-            store_part<D>(p, (int64_t)item * p.tile_pairs + pr, d4, acc, M, l);
-        } else {
-            int32_t hh;
-            const int32_t rr = divide(pair0 + pr, G, hh);
-            hh = query_head(p, head0 + hh);
-            store_pair<D, BF16>(p, (int64_t)(r.row0 + rr) * p.n_q_heads + hh, d4, acc, M, l);
+        if (kg == 0) {
+            lds_ml[wave][u * 16 + l16][0] = m_ref[u];
+            lds_ml[wave][u * 16 + l16][1] = l_run[u];
+        }
+        __syncthreads();
+        const int32_t n = min(n_pairs - u * 16, 16);
+        for (int32_t i = tid; i < n * (D / 4); i += NW * 64) {
+            const int32_t at_o = i / (D / 4), pr = u * 16 + at_o, d4 = i % (D / 4) * 4;
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) M = fmaxf(M, lds_ml[w][pr][0]);
+            const float ref = M == -INFINITY ? 0.f : M;
+            float l = 0.f;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float f = __builtin_amdgcn_exp2f(lds_ml[w][pr][0] - ref);
+                l += f * lds_ml[w][pr][1];
+                acc += f * *reinterpret_cast<const f32x4 *>(all_o + (w * 16 + at_o) * D + d4);
+            }
+            if (at.splits > 1) {
+                store_part<D>(p, (int64_t)item * p.tile_pairs + pr, d4, acc, M, l);
+            } else {
+                int32_t hh;
+                const int32_t rr = divide(pair0 + pr, G, hh);
+                hh = query_head(p, head0 + hh);
+                store_pair<D, BF16>(p, (int64_t)(r.row0 + rr) * p.n_q_heads + hh, d4, acc, M, l);
+            }
         }
     }
 }
@@ -453,14 +487,17 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void merge_kv4_kernel(Kv4
 template <int D, bool BF16, bool FEW>
 static void launch(const Kv4Attn &p, bool merge, hipStream_t stream)
 {
+    const dim3 grid((p.grid + 7) / 8 * 8), block(NW * 64);
     if (p.tile_shift == kKv4RowsTileShift) launch_attn_kv4_rows(p, D, stream);
-    else if (p.shared) hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, FEW, true>), dim3((p.grid + 7) / 8 * 8), dim3(NW * 64), 0, stream, p);
-    else hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, FEW, false>), dim3((p.grid + 7) / 8 * 8), dim3(NW * 64), 0, stream, p);
+    else if (p.tile_shift == kKv4TileShift && !p.shared) hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, 1, false, FEW>), grid, block, 0, stream, p);
+    else if (p.tile_shift == kKv4TileShift) hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, 1, true, FEW>), grid, block, 0, stream, p);
+    else if (!p.shared) hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, 2, false, FEW>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, 2, true, FEW>), grid, block, 0, stream, p);
     if (!merge) return;
     // few units are cut into many items, whose joining is worth more wavefronts where there are few pairs
     const bool long_units = p.max_units <= 16;
     if (!long_units) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 2, FEW>), dim3(p.max_units * ceil_div(p.tile_pairs, 2)), dim3(256), 0, stream, p);
-    else if (p.tile_pairs > kKv4Pairs) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 4, FEW>), dim3(p.max_units * p.tile_pairs), dim3(256), 0, stream, p);
+    else if (p.tile_pairs > 32) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 4, FEW>), dim3(p.max_units * p.tile_pairs), dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16, FEW>), dim3(p.max_units * p.tile_pairs), dim3(1024), 0, stream, p);
 }
 

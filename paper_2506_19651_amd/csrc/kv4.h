@@ -62,7 +62,7 @@ struct Kv4Rows {  // rows of K and V that go into slots, or come out of them
 
 // Attention.  A KV head's (row, query head) pairs of a request, head fastest, are cut into tiles; a unit is one tile against all keys that
 // the request's rows see, in steps of a few records.  Units are cut into items of about equal length: a workgroup takes an item.
-constexpr int32_t kKv4TileShift = 4, kKv4StepShift = 1;          // 16 pairs, 2 records: the kernel of few rows
+constexpr int32_t kKv4TileShift = 4, kKv4StepShift = 1;          // 16 pairs (or twice that), 2 records: the kernel of few rows
 constexpr int32_t kKv4RowsTileShift = 7, kKv4RowsStepShift = 2;  // 128 pairs, 4 records: of many
 
 struct Kv4Heads {
