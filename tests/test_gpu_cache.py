@@ -186,12 +186,12 @@ def test_slots_of_many_requests(n):
 
 # ------------------------------------------------------------------------------------------ attention
 def attn_case(hq, hkv, d, dtype, page, lengths, rows, sink=None, window=None, kv_of_q=None, scale=0.0, seed=0, order=None, edit=None, q_scale=1.0,
-              wide=False):
-    """Makes a cache and queries, calls, and holds out and lse to the oracle.  order: row_start of every request (default: packed); wide: a
-    table of 4096 tokens a request and more, so that with as many (row, head) pairs the kernel of many rows is taken."""
+              wide=None):
+    """Makes a cache and queries, calls, and holds out and lse to the oracle.  order: row_start of every request (default: packed).  wide: how the call
+    is to be cut, "128" for tiles of 128 (row, head) pairs, with a table of 4096 tokens a request and more, "32" for tiles of 32, with one of 2^20."""
     rng = np.random.default_rng(seed + hq + d)
     heads = P.Heads(hq, hkv, d, dtype, kv_of_q, scale)
-    table, pages = pages_for([max(n, 0) for n in lengths], page, rng, width=max(-(-max(lengths) // page), 4096 // page) if wide else None)
+    table, pages = pages_for([max(n, 0) for n in lengths], page, rng, width=max(-(-max(lengths) // page), {"128": 4096, "32": 1 << 20}[wide] // page) if wide else None)
     pool = np.zeros((pages, hkv, page // 16, 17 * d), np.uint8)
     for s, n in enumerate(lengths):
         j = np.arange(max(n, 0))
@@ -212,9 +212,11 @@ def attn_case(hq, hkv, d, dtype, page, lengths, rows, sink=None, window=None, kv
         edit(a)
         q, q64 = q[:a["num_rows"]].contiguous(), q64[:a["num_rows"]]
     if wide:
-        group = max(np.bincount(kv_of_q)) if kv_of_q is not None else hq // hkv
-        pairs = -(-len(q) * group // min(len(rows), len(q)))
-        assert dtype == "bf16" and -(-pairs // 16) > (4 if d == 128 else 7) * -(-pairs // 128)
+        group, asking = max(np.bincount(kv_of_q)) if kv_of_q is not None else hq // hkv, min(len(rows), len(q))
+        tiles16, tiles128 = (-(-len(q) * group // asking // n) for n in (16, 128))
+        many = dtype == "bf16" and tiles16 > (4 if d == 128 else 7) * tiles128
+        steps = asking * tiles16 * hkv * (1 << 15) / ((4 if d == 64 else 3) * torch.cuda.get_device_properties(0).multi_processor_count)
+        assert many if wide == "128" else not many and tiles16 > 1 and steps >= 64
     cache = P.KvCache(torch.from_numpy(a["pool"]).to(DEV), i32(a["table"]), page)
     out = torch.full_like(q, 5.0)
     lse = torch.full(q.shape[:2], 5.0, device=DEV)
@@ -346,8 +348,8 @@ def test_bad_pages_and_lengths(rows, dtype):
     attn_case(8, 2, 64, dtype, 16, [96, 90, 33], rows, edit=negative)
 
 
-@pytest.mark.parametrize("dtype,rows,wide", [("bf16", [1, 1], False), ("f32", [1, 1], False), ("bf16", [3, 40], False), ("f32", [3, 40], False),
-                                             ("bf16", [3, 40], True), ("bf16", [19, 47], True)])
+@pytest.mark.parametrize("dtype,rows,wide", [("bf16", [1, 1], None), ("f32", [1, 1], None), ("bf16", [3, 40], None), ("f32", [3, 40], None),
+                                             ("bf16", [3, 40], "128"), ("bf16", [19, 47], "128"), ("bf16", [6, 7], "32"), ("f32", [19, 47], "32")])
 def test_blocks_without_a_value(dtype, rows, wide):
     """NaN blocks reach the rows that see them: a key's all of the row, a value's its 32 elements; masked ones nobody."""
     def nan_at(a, s, token, which, block):
@@ -380,37 +382,37 @@ def test_blocks_without_a_value(dtype, rows, wide):
 @pytest.mark.parametrize("hq,hkv,d", [(28, 4, 128), (14, 2, 64), (3, 3, 64), (8, 8, 128), (33, 3, 64)])
 @pytest.mark.parametrize("page", [16, 64, 512])
 def test_many_rows(page, hq, hkv, d):
-    attn_case(hq, hkv, d, "bf16", page, [1500], [128], wide=True)
-    attn_case(hq, hkv, d, "bf16", page, [200, 119, 300, 135], [100, 119, 161, 129], wide=True)
+    attn_case(hq, hkv, d, "bf16", page, [1500], [128], wide="128")
+    attn_case(hq, hkv, d, "bf16", page, [200, 119, 300, 135], [100, 119, 161, 129], wide="128")
 
 
 def test_many_rows_with_masks():
     n = [200, 333, 64, 500, 90]
-    attn_case(8, 2, 128, "bf16", 16, n, [40, 64, 70, 33, 80], sink=[0, 16, 300, 5, -3], window=[0, 1, 16, 100, 2 ** 31 - 1], wide=True)
-    attn_case(8, 2, 128, "bf16", 16, n, [40, 64, 60, 33, 80], window=[-1, 50, 64, 65, 63], wide=True)
-    attn_case(14, 2, 64, "bf16", 32, [2500, 700], [77, 130], sink=[100, 17], window=[600, 1], wide=True)
-    want = attn_case(14, 2, 64, "bf16", 16, [30, 0, 320], [150, 2, 250], wide=True)  # more rows than tokens
+    attn_case(8, 2, 128, "bf16", 16, n, [40, 64, 70, 33, 80], sink=[0, 16, 300, 5, -3], window=[0, 1, 16, 100, 2 ** 31 - 1], wide="128")
+    attn_case(8, 2, 128, "bf16", 16, n, [40, 64, 60, 33, 80], window=[-1, 50, 64, 65, 63], wide="128")
+    attn_case(14, 2, 64, "bf16", 32, [2500, 700], [77, 130], sink=[100, 17], window=[600, 1], wide="128")
+    want = attn_case(14, 2, 64, "bf16", 16, [30, 0, 320], [150, 2, 250], wide="128")  # more rows than tokens
     assert (want["keys"][:120] == 0).all() and (want["keys"][150:152] == 0).all() and want["keys"][120] == 1
 
 
 def test_many_rows_of_mapped_heads():
-    attn_case(6, 3, 64, "bf16", 16, [150, 600], [100, 200], kv_of_q=[2, 0, 2, 2, 0, 2], wide=True)
-    attn_case(8, 2, 128, "bf16", 32, [300, 131], [60, 40], kv_of_q=[1, 0, 0, 1, 1, 0, 1, 0], wide=True)
-    attn_case(40, 2, 64, "bf16", 32, [100, 31], [20, 12], kv_of_q=[1] * 39 + [0], scale=0.2, wide=True)
+    attn_case(6, 3, 64, "bf16", 16, [150, 600], [100, 200], kv_of_q=[2, 0, 2, 2, 0, 2], wide="128")
+    attn_case(8, 2, 128, "bf16", 32, [300, 131], [60, 40], kv_of_q=[1, 0, 0, 1, 1, 0, 1, 0], wide="128")
+    attn_case(40, 2, 64, "bf16", 32, [100, 31], [20, 12], kv_of_q=[1] * 39 + [0], scale=0.2, wide="128")
 
 
 def test_many_rows_with_scores_far_apart():
-    attn_case(8, 2, 128, "bf16", 16, [400, 77], [60, 70], q_scale=12.0, wide=True)
-    attn_case(2, 1, 64, "bf16", 16, [1500], [127], scale=6.0, wide=True)
+    attn_case(8, 2, 128, "bf16", 16, [400, 77], [60, 70], q_scale=12.0, wide="128")
+    attn_case(2, 1, 64, "bf16", 16, [1500], [127], scale=6.0, wide="128")
 
 
 def test_many_rows_of_a_padded_batch():
-    attn_case(4, 2, 64, "bf16", 16, [140, 0, 117, 190], [120, 0, 101, 77], order=[380, 360, 0, 200], wide=True)
+    attn_case(4, 2, 64, "bf16", 16, [140, 0, 117, 190], [120, 0, 101, 77], order=[380, 360, 0, 200], wide="128")
 
     def short(a):  # rows that end behind the tensors
         a["num_rows"] = 499
         a["row_start"][:] = [380, 360, 90, -1]
-    attn_case(4, 2, 64, "bf16", 16, [140, 0, 117, 190], [120, 0, 101, 77], order=[380, 360, 0, 200], edit=short, wide=True)
+    attn_case(4, 2, 64, "bf16", 16, [140, 0, 117, 190], [120, 0, 101, 77], order=[380, 360, 0, 200], edit=short, wide="128")
 
 
 def test_many_rows_with_bad_pages_and_lengths():
@@ -419,17 +421,48 @@ def test_many_rows_with_bad_pages_and_lengths():
         a["table"][1, [0, 3]] = [len(a["pool"]), 2 ** 31 - 1]
         a["table"][2, :] = -(2 ** 31)
         a["seq_len"][0] = 2 ** 31 - 1  # as long as the table is wide
-    attn_case(8, 2, 128, "bf16", 16, [96, 90, 33], [40, 90, 60], edit=edit, wide=True)
+    attn_case(8, 2, 128, "bf16", 16, [96, 90, 33], [40, 90, 60], edit=edit, wide="128")
 
     def negative(a):
         a["seq_len"][:] = [-5, 0, 212]
         a["row_len"][1] = -(2 ** 31)
-    attn_case(8, 2, 128, "bf16", 16, [96, 90, 212], [40, 90, 60], edit=negative, wide=True)
+    attn_case(8, 2, 128, "bf16", 16, [96, 90, 212], [40, 90, 60], edit=negative, wide="128")
 
 
 def test_many_requests_with_many_rows():
     rng = np.random.default_rng(6)
-    attn_case(4, 1, 128, "bf16", 16, rng.integers(1, 100, 150).tolist(), rng.integers(20, 40, 150).tolist(), wide=True)
+    attn_case(4, 1, 128, "bf16", 16, rng.integers(1, 100, 150).tolist(), rng.integers(20, 40, 150).tolist(), wide="128")
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d", [(28, 4, 128), (14, 2, 64), (32, 1, 128), (24, 3, 64)])
+def test_tiles_of_32(hq, hkv, d, dtype):
+    attn_case(hq, hkv, d, dtype, 64, [700, 31, 300, 33], [2, 2, 1, 3] if hkv == 1 else [3, 5, 1, 8], wide="32")
+    attn_case(hq, hkv, d, dtype, 512, [1500], [31 * hkv // hq + 2], wide="32")
+    if dtype == "f32":
+        attn_case(hq, hkv, d, dtype, 64, [300, 119], [60, 119], wide="32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tiles_of_32_with_masks(dtype):
+    n = [200, 333, 64, 500, 90]
+    attn_case(8, 2, 128, dtype, 64, n, [4, 9, 12, 10, 17], sink=[0, 16, 300, 5, -3], window=[0, 1, 16, 100, 2 ** 31 - 1], wide="32")
+    attn_case(14, 2, 64, dtype, 64, [900, 700], [9, 5], sink=[100, 17], window=[600, 1], wide="32")
+    want = attn_case(14, 2, 64, dtype, 64, [3, 0, 320], [15, 2, 5], wide="32")  # more rows than tokens
+    assert (want["keys"][:12] == 0).all() and want["keys"][12] == 1
+    attn_case(6, 3, 64, dtype, 64, [50, 200], [13, 9], kv_of_q=[2, 0, 2, 2, 0, 2], wide="32")
+    attn_case(8, 2, 128, dtype, 64, [400, 77], [6, 7], q_scale=12.0, wide="32")
+
+    def short(a):  # rows that end behind the tensors
+        a["num_rows"] = 40
+        a["row_start"][:] = [30, 20, 10, -1]
+    attn_case(8, 2, 64, dtype, 64, [40, 0, 17, 90], [11, 0, 6, 7], order=[30, 20, 0, 10], edit=short, wide="32")
+
+    def bad(a):
+        a["table"][0, 2] = -1
+        a["table"][1, [0, 3]] = [len(a["pool"]), 2 ** 31 - 1]
+        a["seq_len"][2] = -5
+    attn_case(8, 2, 64, dtype, 16, [96, 90, 33], [6, 8, 7], edit=bad, wide="32")
+
 
 
 def test_lengths_of_many_millions():
