@@ -356,7 +356,8 @@ size_t pevlm_cache_pool_bytes(const pevlm_heads *heads, int32_t num_pages, int32
  *   block_table                gets the new pages; other entries stay as they are
  * A request is not served, and keeps what it has, if it would outgrow its row of the table, if its rows end behind num_rows, or
  * if the list does not hold the pages that it and those of the requests before it need that fit otherwise.
- * num_free is taken within [0, free_capacity], seq_len from 0 on.  Workspace: pevlm_cache_slots_workspace_bytes.
+ * num_free is taken within [0, free_capacity], seq_len from 0 on.  num_rows: at most 2^30.  Workspace:
+ * pevlm_cache_slots_workspace_bytes.
  */
 size_t pevlm_cache_slots_workspace_bytes(int32_t num_seqs);
 pevlm_status pevlm_cache_slots(const pevlm_cache *cache, const int32_t *seq_len, const int32_t *new_len, const int32_t *free_pages,
@@ -368,7 +369,8 @@ pevlm_status pevlm_cache_slots(const pevlm_cache *cache, const int32_t *seq_len,
  * K and V of num_rows tokens into the slots slot_map names (rows whose slot is outside the pool, as -1 is, go nowhere; the slots of
  * a call are distinct), and the values of such slots back (rows without a slot are left as they were).  Rows of k and v are [Hkv][D]
  * of heads->dtype, k_stride and v_stride elements apart (0: contiguous; otherwise at least Hkv * D and a multiple of 8), bases 16-byte
- * aligned.  K is kept as given, so it is rotated first.  Of heads only n_kv_heads, head_dim and dtype matter.  block_table may be NULL.
+ * aligned.  A launch has fewer than 2^32 lanes, which bounds num_rows * Hkv (2^30 for head_dim 128, 2^31 for 64; more: PEVLM_ERR_UNSUPPORTED);
+ * num_rows: at most 2^30.  K is kept as given, so it is rotated first.  Of heads only n_kv_heads, head_dim and dtype matter.  block_table may be NULL.
  */
 pevlm_status pevlm_cache_store_kv4(const void *k, const void *v, int64_t k_stride, int64_t v_stride, const int32_t *slot_map, int32_t num_rows,
                                    const pevlm_cache *cache, const pevlm_heads *heads, void *stream);
@@ -386,7 +388,8 @@ pevlm_status pevlm_cache_load_kv4(void *k, void *v, int64_t k_stride, int64_t v_
  * pages without a visible token are not read.  Several requests may name the same pages, no two the same rows.
  *
  * The keys of a request are split over workgroups, and the parts merged, by the lengths of all requests: results are the same
- * for the same arguments, not for a request in another batch.  Workspace: pevlm_cache_attn_workspace_bytes.
+ * for the same arguments, not for a request in another batch.  More than about 2^25 (row, query head) pairs are refused
+ * (PEVLM_ERR_UNSUPPORTED: 2^32 lanes a launch).  Workspace: pevlm_cache_attn_workspace_bytes.
  */
 size_t pevlm_cache_attn_workspace_bytes(const pevlm_heads *heads, int32_t num_seqs, int32_t num_rows);
 pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pevlm_cache *cache, const pevlm_heads *heads, int32_t num_rows,

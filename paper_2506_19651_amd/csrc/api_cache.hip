@@ -8,6 +8,9 @@
 
 namespace pevlm {
 
+constexpr int64_t kMaxThreads = (int64_t)1 << 32;  // of a launch: fewer
+constexpr int32_t kMaxRows = 1 << 30;              // a row's number and a few more fit 32 bits
+
 constexpr int32_t kMinPage = 16, kMaxPage = 4096;
 constexpr int32_t kMaxTokens = 1 << 30;  // of a request: a token's place and a tile's length add up in 32 bits
 
@@ -51,6 +54,8 @@ static pevlm_status check_rows(const void *k, const void *v, int64_t k_stride, i
     st = check_pool(cache, &p->pool, heads->n_kv_heads);
     if (st != PEVLM_OK) return st;
     if (num_rows < 0) return fail(PEVLM_ERR_INVALID_ARG, "num_rows must not be negative");
+    if (num_rows > kMaxRows || ((int64_t)num_rows / kv4_rows_of_wave(heads->head_dim) + 1) * heads->n_kv_heads * 64 + 256 > kMaxThreads)
+        return fail(PEVLM_ERR_UNSUPPORTED, "too many rows: %d of %d heads", num_rows, heads->n_kv_heads);
     const int64_t row = (int64_t)heads->n_kv_heads * heads->head_dim;
     for (int64_t stride : {k_stride, v_stride})
         if (stride != 0 && (stride < row || stride % 8 != 0 || stride > INT32_MAX))
@@ -169,6 +174,7 @@ pevlm_status pevlm_cache_slots(const pevlm_cache *cache, const int32_t *seq_len,
     if (st == PEVLM_OK) st = check_table(cache);
     if (st != PEVLM_OK) return st;
     if (num_rows < 0 || free_capacity < 0) return fail(PEVLM_ERR_INVALID_ARG, "num_rows and free_capacity must not be negative");
+    if (num_rows > kMaxRows) return fail(PEVLM_ERR_UNSUPPORTED, "too many rows: %d", num_rows);
     if (!seq_len || !num_free || !seq_len_out || !num_free_out || !row_start || !row_len || (!free_pages && free_capacity > 0) || (!slot_map && num_rows > 0))
         return fail(PEVLM_ERR_INVALID_ARG, "only new_len, pos_offset and pos_ids (and arrays without an entry) may be NULL");
     for (const int32_t *a : {seq_len, new_len, free_pages, num_free, pos_offset, (const int32_t *)seq_len_out, (const int32_t *)num_free_out,
@@ -252,7 +258,15 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
         if (!aligned4(a)) return fail(PEVLM_ERR_INVALID_ARG, "arrays must be 4-byte aligned");
     const int64_t width = (int64_t)cache->max_pages * cache->page_size;
     size_attn(heads, tab, cache->num_seqs, num_rows, cut_of(heads, group_heads(tab, heads, &p.heads), cache->num_seqs, num_rows, width), &p);
-    if (p.max_items > 0x3fffffff || ((int64_t)p.max_units << p.tile_shift) > 1 << 30) return fail(PEVLM_ERR_UNSUPPORTED, "too many work items");
+    // no request is longer than its row of the table
+    const int64_t step = kKv4Record << p.step_shift, longest = ((width + step - 1) / step + p.min_steps - 1) / p.min_steps;
+    const int64_t grid = (std::min<int64_t>(p.max_items, p.max_units * longest) + 7) / 8 * 8;  // in eighths of the XCDs
+    // Few units are cut into many items, whose joining is worth more wavefronts where there are few pairs, 2 / 16 of them: one request of 65.9 K tokens, 1
+    // row 25.5 / 19.9 us, 2 rows 27.0 / 21.5, 8 rows 32.7 / 32.8, 40 rows 62.8 / 76.4; 4 requests 39.0 / 39.9, 16 102 / 118
+    p.merge_waves = p.max_units <= 16 && p.tile_pairs <= 32 ? 16 : 2;
+    const int64_t merge_grid = longest > 1 ? (int64_t)p.max_units * (p.merge_waves == 2 ? ceil_div(p.tile_pairs, 2) : p.tile_pairs) : 0;
+    if (((int64_t)p.max_units << p.tile_shift) > kMaxRows || grid * 256 >= kMaxThreads || merge_grid * (p.merge_waves == 16 ? 1024 : 256) >= kMaxThreads)
+        return fail(PEVLM_ERR_UNSUPPORTED, "too many rows: %d of %d heads", num_rows, heads->n_q_heads);
     const size_t need = attn_bytes(p, heads->head_dim);
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))
         return fail(PEVLM_ERR_WORKSPACE_TOO_SMALL, "cache attention workspace needs %zu bytes, 256-byte aligned (got %zu)",
@@ -265,12 +279,11 @@ pevlm_status pevlm_cache_attn_kv4(const void *q, void *out, float *lse, const pe
     p.num_rows = num_rows;
     p.n_q_heads = heads->n_q_heads;
     p.part_ml = (float *)workspace;
-    // no request is longer than its row of the table
-    const int64_t longest = ceil_div((int32_t)((width + (kKv4Record << p.step_shift) - 1) / (kKv4Record << p.step_shift)), p.min_steps);
-    p.grid = (int32_t)std::min<int64_t>(p.max_items, p.max_units * longest);
+    p.grid = (int32_t)grid;
+    p.merge_grid = (int32_t)merge_grid;
     p.part_acc = (float *)((char *)workspace + ml_bytes(p));
     p.c_log2 = scale_of(heads) * 1.4426950408889634f;
-    const hipError_t e = launch_attn_kv4(p, heads->head_dim, heads->dtype == PEVLM_BF16, longest > 1, (hipStream_t)stream);
+    const hipError_t e = launch_attn_kv4(p, heads->head_dim, heads->dtype == PEVLM_BF16, (hipStream_t)stream);
     return e == hipSuccess ? PEVLM_OK : hip_fail(e, "cache attention launch");
 }
 

@@ -151,6 +151,7 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
     Place at;
     at.s = -1;
     at.first_item = 0;
+    if (!UNITS && idx >= p.max_items) return at;  // row ranges that overlap can make more: no place in the workspace
     if (SHARED) {
         int32_t all = 0;
         for (int32_t s0 = 0; s0 < (FEW ? 1 : p.num_seqs); s0 += 64) {

@@ -8,7 +8,14 @@
 // the wavefront's own and back transposed (ds_read_b64_tr_b16).
 //
 // Roundings: Q of fp32 tensors is split into three bf16 parts that add up to it, weights into two (bf16 tensors, 2^-16) or three
-// parts (fp32); products of parts are exact in fp32, sums are fp32 throughout.
+// parts (fp32); products of parts are exact in fp32, sums are fp32 throughout.  (Weights of one part save 2 %: 101 -> 99 us for 16 requests of 65.9 K
+// tokens.)
+//
+// A workgroup of four wavefronts takes an item, a run of steps of 32 tokens, the wavefronts in turn; what they have is joined in LDS.  Bound by HBM
+// where there are many items: 16 requests of 65.9 K tokens x 28/4 heads x 128 (577 MB) 98 us, 5.9 TB/s with both launches, 6.3 inside the kernel;
+// with all codes in the caches its arithmetic takes 60 of them (vector instructions issue 61 %, matrix cores are busy 27 % of the time).  One request of 65.9 K tokens
+// (36 MB) is a chain of round trips, 18.7 us: fields, lengths, table, records (3 us), three steps (5), the join (1), launch and merge (9).  Three
+// workgroups a compute unit are enough (four 101.6 against 100.9 us, two 111), and two steps ahead are no faster than one.
 #include "attn_kv4.h"
 
 namespace pevlm {
@@ -48,7 +55,7 @@ constexpr float kStep = 8.f;  // base-2 units that a row's maximum may outgrow i
 
 }  // namespace
 
-// PT: tiles of 16 pairs that share the decoded records; SHARED: whether other workgroups read the same codes
+// PT: tiles of 16 pairs that share the decoded records; SHARED: whether other workgroups read the same codes; FEW: up to 64 requests
 template <int D, bool BF16, int PT, bool SHARED, bool FEW>
 __global__ __launch_bounds__(NW * 64, PT == 1 ? 3 : 2) void attn_kv4_kernel(Kv4Attn p)
 {
@@ -382,10 +389,10 @@ __global__ __launch_bounds__(NW * 64, PT == 1 ? 3 : 2) void attn_kv4_kernel(Kv4A
     }
 }
 
-// Joins the items of the units that were cut.  WAVES wavefronts take a pair, a workgroup of 256 or more lanes one or two pairs of a unit:
-// D / 4 lanes cover a row of values and the groups of them take the items in turn, kTurn at once with their maxima and sums, against a
-// running maximum of their own; then the groups are joined.  A lane that walks all items takes a memory round trip for each (23 us for 128 items
-// of 28 pairs), and to fetch all maxima before the first values is one round trip more.
+// Joins the items of the units that were cut.  WAVES wavefronts take a pair, a workgroup one (16) or two (2) pairs of a unit: D / 4 lanes cover a row of
+// values and the groups of them take the items in turn, kTurn at once with their maxima and sums, against a running maximum of their own; then
+// the groups are joined.  Bound by latency, 4 to 5 us: the lengths, then the parts, in one memory round trip each.  (Lanes that walk all items take a
+// trip for each, 23 us for 128 items of 28 pairs, and to fetch all maxima before the first values is one trip more.)
 constexpr int kTurn = 6;
 
 template <int D, bool BF16, int WAVES, bool FEW>
@@ -485,32 +492,29 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void merge_kv4_kernel(Kv4
 }
 
 template <int D, bool BF16, bool FEW>
-static void launch(const Kv4Attn &p, bool merge, hipStream_t stream)
+static void launch(const Kv4Attn &p, hipStream_t stream)
 {
-    const dim3 grid((p.grid + 7) / 8 * 8), block(NW * 64);
+    const dim3 grid(p.grid), block(NW * 64);
     if (p.tile_shift == kKv4RowsTileShift) launch_attn_kv4_rows(p, D, stream);
     else if (p.tile_shift == kKv4TileShift && !p.shared) hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, 1, false, FEW>), grid, block, 0, stream, p);
     else if (p.tile_shift == kKv4TileShift) hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, 1, true, FEW>), grid, block, 0, stream, p);
     else if (!p.shared) hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, 2, false, FEW>), grid, block, 0, stream, p);
     else hipLaunchKernelGGL((attn_kv4_kernel<D, BF16, 2, true, FEW>), grid, block, 0, stream, p);
-    if (!merge) return;
-    // few units are cut into many items, whose joining is worth more wavefronts where there are few pairs
-    const bool long_units = p.max_units <= 16;
-    if (!long_units) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 2, FEW>), dim3(p.max_units * ceil_div(p.tile_pairs, 2)), dim3(256), 0, stream, p);
-    else if (p.tile_pairs > 32) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 4, FEW>), dim3(p.max_units * p.tile_pairs), dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16, FEW>), dim3(p.max_units * p.tile_pairs), dim3(1024), 0, stream, p);
+    if (p.merge_grid == 0) return;
+    if (p.merge_waves == 2) hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 2, FEW>), dim3(p.merge_grid), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16, FEW>), dim3(p.merge_grid), dim3(1024), 0, stream, p);
 }
 
 template <int D, bool BF16>
-static void launch(const Kv4Attn &p, bool merge, hipStream_t stream)
+static void launch(const Kv4Attn &p, hipStream_t stream)
 {
-    p.num_seqs <= 64 ? launch<D, BF16, true>(p, merge, stream) : launch<D, BF16, false>(p, merge, stream);
+    p.num_seqs <= 64 ? launch<D, BF16, true>(p, stream) : launch<D, BF16, false>(p, stream);
 }
 
-hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, bool merge, hipStream_t stream)
+hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, hipStream_t stream)
 {
-    if (D == 128) bf16 ? launch<128, true>(p, merge, stream) : launch<128, false>(p, merge, stream);
-    else bf16 ? launch<64, true>(p, merge, stream) : launch<64, false>(p, merge, stream);
+    if (D == 128) bf16 ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
+    else bf16 ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
     return hipGetLastError();
 }
 

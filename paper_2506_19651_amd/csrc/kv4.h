@@ -60,6 +60,9 @@ struct Kv4Rows {  // rows of K and V that go into slots, or come out of them
     Kv4Pool pool;
 };
 
+// Rows of one KV head that a wavefront takes in or out: four loads of 8 elements a lane
+constexpr int32_t kv4_rows_of_wave(int32_t D) { return 4 * 64 / (D / 8); }
+
 // Attention.  A KV head's (row, query head) pairs of a request, head fastest, are cut into tiles; a unit is one tile against all keys that
 // the request's rows see, in steps of a few records.  Units are cut into items of about equal length: a workgroup takes an item.
 constexpr int32_t kKv4TileShift = 4, kKv4StepShift = 1;          // 16 pairs (or twice that), 2 records: the kernel of few rows
@@ -86,6 +89,7 @@ struct Kv4Attn {
     int32_t target, min_steps;        // items that a call is cut into, if they are not shorter than this
     int32_t max_items, max_units;     // bounds that no lengths pass
     int32_t grid;                     // and one for the items that the table's width allows
+    int32_t merge_waves, merge_grid;  // of the kernel that joins items: wavefronts of a pair, workgroups (0: no unit is cut)
     float c_log2;                     // softmax scale * log2(e)
     Kv4Heads heads;
 };
@@ -94,6 +98,6 @@ hipError_t launch_kv4_slots(const Kv4Slots &p, hipStream_t stream);
 hipError_t launch_kv4_store(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream);
 hipError_t launch_kv4_load(const Kv4Rows &p, int32_t D, bool bf16, hipStream_t stream);
 void launch_attn_kv4_rows(const Kv4Attn &p, int32_t D, hipStream_t stream);  // bf16 tensors
-hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, bool merge, hipStream_t stream);
+hipError_t launch_attn_kv4(const Kv4Attn &p, int32_t D, bool bf16, hipStream_t stream);
 
 }  // namespace pevlm

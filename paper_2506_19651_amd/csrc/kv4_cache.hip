@@ -8,7 +8,7 @@ namespace pevlm {
 // Slots.  What a request gets depends on those before it only through two running sums (rows, pages), so one workgroup
 // takes the requests T at a time: inclusive scans of the new tokens, then of the pages that the requests which fit lack.  Sums stop
 // at 2^32 - 1, which is more than any bound they are held to.  A step's few rows are filled in by the same workgroup from LDS; a prompt's by
-// a launch of one row a lane.  Bound by latency: kernel 4.2 us for 64 requests of one token where two launches took 3.9 and 2.6.
+// a launch of one row a lane.  Bound by latency: 2.9 us for 64 requests of one token, 2.8 and 4.1 for four prompts of 141 K tokens.
 // ------------------------------------------------------------------------------------------
 constexpr int32_t kSmallRows = 2048, kSmallRequests = 1024;
 
@@ -157,13 +157,14 @@ hipError_t launch_kv4_slots(const Kv4Slots &p, hipStream_t stream)
 // Rows in and out.  A wavefront takes kRowsAt rows of one KV head, K and V.  A lane has 8 neighbouring elements of a row (chunk
 // l % (D / 8)), so that the wavefront's loads cover whole rows; four lanes make a block and find its scale.  What lane c of the four
 // encodes of their four rows is one word of each row's 16 bytes: a transpose within the four gives every lane the 16 bytes of one row,
-// and a wavefront's store is a record's codes as they lie, if its rows are neighbours in the cache.  Out the same way back.  Bound by HBM.
+// and a wavefront's store is a record's codes as they lie, if its rows are neighbours in the cache.  Out the same way back.  Bound by HBM:
+// 65.9 K tokens x 4 heads x 128 in 31.0 us, out 27.6 (171 MB each, 5.5 and 6.2 TB/s), 100 K x 8 out 96 (524 MB, 5.4).
 // ------------------------------------------------------------------------------------------
 template <int D>
 struct RowsCfg {
     static constexpr int CH = D / 8;        // chunks of a row
     static constexpr int PER_LOAD = 64 / CH; // rows that one load of 8 elements a lane covers
-    static constexpr int ROWS = 4 * PER_LOAD;
+    static constexpr int ROWS = kv4_rows_of_wave(D);
 };
 
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E;  // quad_perm of the neighbour, and of the one after the next

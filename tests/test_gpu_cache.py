@@ -465,6 +465,25 @@ def test_tiles_of_32_with_masks(dtype):
 
 
 
+@pytest.mark.parametrize("width,rows", [(64, 3), (8192, 3), (8192, 70), (1 << 20, 9)])
+def test_requests_that_name_the_same_rows_write_nothing_else(width, rows):
+    """Not allowed, and their rows hold no result; but nothing outside the tensors and the workspace is written."""
+    heads, n, page = P.Heads(8, 2, 128, "bf16"), 700, 64
+    pool = torch.zeros((4, 2, 4, 17 * 128), dtype=torch.uint8, device=DEV)
+    cache = P.KvCache(pool, torch.zeros((n, width // page), dtype=torch.int32, device=DEV), page)
+    need = P.pevlm_cache_attn_workspace_bytes(heads, n, rows)
+    block = torch.full((need + (1 << 20),), 77, dtype=torch.uint8, device=DEV)
+    around = torch.full((rows + 64, 8, 128), 5.0, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((rows + 64, 8), 5.0, device=DEV)
+    q = torch.randn((rows, 8, 128), device=DEV).bfloat16()
+    for per in (rows, 1):
+        P.pevlm_cache_attn_kv4(q, around[32:32 + rows], cache, heads, i32([0] * n), i32([per] * n), i32([2 ** 31 - 1] * n), lse=lse[32:32 + rows],
+                               workspace=block[:need])
+    torch.cuda.synchronize()
+    assert (block[need:] == 77).all() and (around[:32] == 5).all() and (around[32 + rows:] == 5).all()
+    assert (lse[:32] == 5).all() and (lse[32 + rows:] == 5).all()
+
+
 def test_lengths_of_many_millions():
     """Every page of the table is the same one: the rows before the last see n copies of its tokens, so out is that of one page and lse more by log(n)."""
     page, width = 4096, 1 << 13  # 2^25 tokens

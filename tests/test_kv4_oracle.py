@@ -174,6 +174,20 @@ def test_attention_refuses_bad_arguments():
     assert P.pevlm_cache_attn_workspace_bytes(heads, 0, 1) == 0 and P.pevlm_cache_attn_workspace_bytes(heads, 1, -1) == 0
 
 
+def test_more_rows_than_a_launch_has_lanes_are_refused():
+    lib = P.load_library()
+    for d, hkv, rows in ((128, 8, 1 << 27), (64, 8, 1 << 28), (64, 1, (1 << 30) + 1), (64, 1, 2 ** 31 - 1)):
+        for fn in (lib.pevlm_cache_store_kv4, lib.pevlm_cache_load_kv4):
+            assert fn(FAKE, FAKE, 0, 0, FAKE, rows, _cache(), P.Heads(8, hkv, d, "bf16").ref(), None) == UNSUPPORTED, (d, hkv, rows)
+    for rows in ((1 << 30) + 1, 2 ** 31 - 1):
+        assert lib.pevlm_cache_slots(_cache(), FAKE, None, FAKE, 3, FAKE, rows, None, FAKE, FAKE, FAKE, FAKE, FAKE, None, FAKE, 1 << 20, None) == UNSUPPORTED
+    for hq, hkv, d, dtype, width in ((32, 8, 128, "bf16", 16), (32, 1, 64, "bf16", 1 << 12), (8, 8, 128, "f32", 1 << 12)):
+        cache = _cache(max_pages=width // 16 * 16)
+        for rows in (1 << 25, 2 ** 31 - 1):
+            assert lib.pevlm_cache_attn_kv4(FAKE, FAKE, None, cache, P.Heads(hq, hkv, d, dtype).ref(), rows, FAKE, FAKE, FAKE, None, None, FAKE, 1 << 62,
+                                            None) == UNSUPPORTED, (hq, hkv, d, dtype, rows)
+
+
 def test_pool_bytes():
     assert P.pevlm_cache_pool_bytes(P.Heads(28, 4, 128, "bf16"), 10, 64) == 10 * 64 * 4 * 136
     assert P.pevlm_cache_pool_bytes(P.Heads(14, 2, 64, "f32"), 3, 16) == 3 * 16 * 2 * 68
