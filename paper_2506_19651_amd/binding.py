@@ -676,6 +676,8 @@ def _kv_rows(cache: KvCache, heads: Heads, k, v, slot_map):
         stride = t.stride()
         if (stride[2] != 1 or (stride[1] != inner and shape[1] > 1)) and rows:
             _refuse(f"a row of {name} must be contiguous (strides {stride})")
+        if rows > 1 and stride[0] < shape[1] * inner:  # 0, of an expanded tensor, would say contiguous to the library
+            _refuse(f"rows of {name} must lie at least {shape[1] * inner} elements apart (strides {stride})")
         if t.get_device() != device:
             _refuse(f"{name} is on {t.device}, the cache on device {device}")
         args.append((t.data_ptr(), stride[0] if rows > 1 else 0))

@@ -227,3 +227,17 @@ def test_the_binding_refuses_what_the_tensors_say():
         args[at] = args[at].float() if at != 2 else args[at].long()
         with pytest.raises(P.PevlmError):
             P.pevlm_cache_slots(cache, *args, i32(9), workspace=ok["workspace"])
+
+
+def test_the_binding_refuses_rows_that_share_memory():
+    """A row stride of 0 means contiguous rows to the library: one row that stands for five must not get there."""
+    heads = P.Heads(4, 2, 64, "bf16")
+    cache = P.KvCache(P.KvCache.new_pool(heads, 3, 32, "cpu"), torch.zeros((2, 4), dtype=torch.int32), 32)
+    k, slots = torch.zeros((5, 2, 64), dtype=torch.bfloat16), torch.zeros(5, dtype=torch.int32)
+    one = torch.zeros((1, 2, 64), dtype=torch.bfloat16).expand(5, 2, 64)
+    near = torch.zeros(5 * 128, dtype=torch.bfloat16).as_strided((5, 2, 64), (64, 64, 1))
+    for bad in (one, near):
+        for args in ((bad, k), (k, bad)):
+            for call in (P.pevlm_cache_store_kv4, P.pevlm_cache_load_kv4):
+                with pytest.raises(P.PevlmError, match="apart"):
+                    call(*args, slots, cache, heads)
