@@ -668,7 +668,7 @@ def _kv_rows(cache: KvCache, heads: Heads, k, v, slot_map):
     """Arguments of the calls that move rows: k and v [rows][Hkv][D], whose rows may lie further apart."""
     _check_heads_of(cache, heads)
     int32, dtypes, _f32, _u8, _current, _raw = _TORCH or _torch()
-    rows, dtype, inner = slot_map.numel(), dtypes[heads.struct.dtype], cache.head_dim
+    rows, dtype, inner = slot_map.numel(), dtypes.get(heads.struct.dtype), cache.head_dim
     shape, device, args = (rows, cache.n_kv_heads, inner), cache.device, []
     for name, t in (("k", k), ("v", v)):
         if t.dtype is not dtype or t.shape != shape:
@@ -705,7 +705,7 @@ def pevlm_cache_attn_kv4(q, out, cache: KvCache, heads: Heads, row_start, row_le
     _check_heads_of(cache, heads)
     int32, dtypes, f32, _u8, _current, _raw = _TORCH or _torch()
     n, rows, device = cache.num_seqs, q.shape[0], cache.device
-    shape, dtype = (rows, heads.n_q_heads, heads.head_dim), dtypes[heads.struct.dtype]
+    shape, dtype = (rows, heads.n_q_heads, heads.head_dim), dtypes.get(heads.struct.dtype)
     for name, t in (("q", q), ("out", out)):
         if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
             _refuse(f"{name} must be contiguous, {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype}")

@@ -241,3 +241,15 @@ def test_the_binding_refuses_rows_that_share_memory():
             for call in (P.pevlm_cache_store_kv4, P.pevlm_cache_load_kv4):
                 with pytest.raises(P.PevlmError, match="apart"):
                     call(*args, slots, cache, heads)
+
+
+def test_the_binding_refuses_a_dtype_that_no_tensor_has():
+    heads = P.Heads(4, 2, 64, 7)
+    cache = P.KvCache(P.KvCache.new_pool(P.Heads(4, 2, 64, "bf16"), 3, 32, "cpu"), torch.zeros((2, 4), dtype=torch.int32), 32)
+    rows, ints = torch.zeros((5, 2, 64), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    q = torch.zeros((5, 4, 64), dtype=torch.bfloat16)
+    for call in (P.pevlm_cache_store_kv4, P.pevlm_cache_load_kv4):
+        with pytest.raises(P.PevlmError):
+            call(rows, rows, torch.zeros(5, dtype=torch.int32), cache, heads)
+    with pytest.raises(P.PevlmError):
+        P.pevlm_cache_attn_kv4(q, q, cache, heads, ints, ints, ints, workspace=torch.zeros(256, dtype=torch.uint8))
