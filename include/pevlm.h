@@ -385,7 +385,7 @@ pevlm_status pevlm_cache_load_kv4(void *k, void *v, int64_t k_stride, int64_t v_
  * (window NULL: all of them; sink_len NULL: 0): a sliding window and first tokens that stay visible.  Tokens on a page outside
  * the pool are not seen.  A row that sees nothing gets zeros, and -inf in lse.  Rows of no request are left as they were, and so are those of a
  * request whose rows do not lie within [0, num_rows).  seq_len is taken within [0, max_pages * page_size].  Table entries of
- * pages without a visible token are not read.  Several requests may name the same pages, no two the same rows.
+ * pages without a visible token do not matter.  Several requests may name the same pages, no two the same rows.
  *
  * The keys of a request are split over workgroups, and the parts merged, by the lengths of all requests: results are the same
  * for the same arguments, not for a request in another batch.  More than about 2^25 (row, query head) pairs are refused
