@@ -34,10 +34,11 @@ __device__ __forceinline__ Request read_request(const Kv4Attn &p, int32_t s)
     return r;
 }
 
-// First token inside the window of the token at position `pos`.  (Where the difference wraps, pos is negative and nothing is seen.)
+// First token inside the window of the token at position `pos`.  A row before the first token (pos < 0) sees nothing, but a tile's or a request's first
+// row sets the edge for those behind it: there it is token 0's, which no later row's lies before and whose difference fits 32 bits.
 __device__ __forceinline__ int32_t near_of(const Request &r, int32_t pos)
 {
-    const int32_t n = (int32_t)((uint32_t)pos - (uint32_t)r.window + 1u);
+    const int32_t n = (int32_t)((uint32_t)max(pos, 0) - (uint32_t)r.window + 1u);
     return r.window < 0 || n < 0 ? 0 : (n < r.held ? n : r.held);
 }
 
