@@ -103,6 +103,9 @@ struct Place {
 template <bool UNITS, bool FEW, bool SHARED = false>
 __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
 {
+#pragma clang fp contract(off)
+    // The attention and the merge find the items' length each for itself, and must agree: every product below is rounded before it is added, which the
+    // compiler would otherwise choose kernel by kernel.
     const int32_t lane = threadIdx.x & 63;
     Request r;
     int32_t steps = 0, tiles = 0;
