@@ -134,10 +134,13 @@ static void size_attn(const pevlm_heads *h, const HeadTable &tab, int32_t num_se
     const int64_t units = h->n_kv_heads * (asking + (pairs >> p->tile_shift));
     p->max_units = (int32_t)std::min<int64_t>(units, INT32_MAX);
     p->max_items = (int32_t)std::min<int64_t>(units + p->target + 8, INT32_MAX);
+    // An item's length is at least work / target, so a unit that is cut, longer than that, has at most twice its share of the target in items (and 64: what
+    // sums round off).  Whole units need no room: 32768 rows of 28/4 heads x 128 in one request are 7168 of them, 480 MiB if they had.
+    p->max_parts = std::min(p->max_items, 2 * p->target + 64);
 }
 
-static size_t ml_bytes(const Kv4Attn &p) { return align256((size_t)p.max_items * p.tile_pairs * 2 * sizeof(float)); }
-static size_t attn_bytes(const Kv4Attn &p, int32_t D) { return ml_bytes(p) + align256((size_t)p.max_items * p.tile_pairs * D * sizeof(float)); }
+static size_t ml_bytes(const Kv4Attn &p) { return align256((size_t)p.max_parts * p.tile_pairs * 2 * sizeof(float)); }
+static size_t attn_bytes(const Kv4Attn &p, int32_t D) { return ml_bytes(p) + align256((size_t)p.max_parts * p.tile_pairs * D * sizeof(float)); }
 
 }  // namespace pevlm
 

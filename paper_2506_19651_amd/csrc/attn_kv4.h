@@ -89,14 +89,14 @@ __device__ __forceinline__ void have_fields(const Kv4Attn &p)
     asm volatile("" ::"s"(p.q), "s"(p.out), "s"(p.lse), "s"(p.pool.base), "s"(p.pool.num_pages), "s"(p.pool.page_shift), "s"(p.pool.n_kv_heads), "s"(p.table),
                  "s"(p.row_start), "s"(p.row_len), "s"(p.seq_len), "s"(p.sink_len), "s"(p.window), "s"(p.part_acc), "s"(p.part_ml), "s"(p.num_seqs),
                  "s"(p.max_pages), "s"(p.num_rows), "s"(p.n_q_heads), "s"(p.tile_pairs), "s"(p.group), "s"(p.mapped), "s"(p.target),
-                 "s"(p.min_steps), "s"(p.max_items), "s"(p.c_log2));
+                 "s"(p.min_steps), "s"(p.max_items), "s"(p.max_parts), "s"(p.c_log2));
 }
 
 // Where the idx-th item (or unit) of a call lies.  Every wavefront finds its own by itself: lane by lane over 64 requests at a
 // time, once for the whole work, which sets the items' length, and once for the place.  FEW: up to 64 requests, which the lanes keep; SHARED:
 // contiguous eighths of the items go to the XCDs, as tiles of the same keys are neighbours.
 struct Place {
-    int32_t s, first_item, splits, tiles, rest;  // rest: the item's (unit's) place within the request
+    int32_t s, first_part, splits, tiles, rest;  // first_part: parts of the requests before; rest: the item's (unit's) place within the request
     Request r;
 };
 
@@ -154,8 +154,7 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
 
     Place at;
     at.s = -1;
-    at.first_item = 0;
-    if (!UNITS && idx >= p.max_items) return at;  // row ranges that overlap can make more: no place in the workspace
+    at.first_part = 0;
     if (SHARED) {
         int32_t all = 0;
         for (int32_t s0 = 0; s0 < (FEW ? 1 : p.num_seqs); s0 += 64) {
@@ -171,7 +170,7 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
     for (int32_t s0 = 0; s0 < (FEW ? 1 : p.num_seqs); s0 += 64) {
         if (!FEW) look(s0 + lane);
         const int32_t splits = splits_of(), items = count(splits), mine = UNITS ? count(1) : items;
-        const int32_t end = wave_scan(mine, sum), item_end = UNITS ? wave_scan(items, sum) : end;
+        const int32_t parts = splits > 1 ? items : 0, end = wave_scan(mine, sum), part_end = wave_scan(parts, sum);
         const uint64_t found = __ballot(sum(before, end) > idx);
         if (found) {
             const int32_t f = __builtin_ctzll(found);
@@ -179,7 +178,8 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
             at.rest = idx - before - (lane_value(end, f) - lane_value(mine, f));
             at.splits = lane_value(splits, f);
             at.tiles = lane_value(tiles, f);
-            at.first_item = sum(at.first_item, lane_value(item_end, f) - lane_value(items, f));
+            at.first_part = sum(at.first_part, lane_value(part_end, f) - lane_value(parts, f));
+            if (!UNITS && at.splits > 1 && sum(at.first_part, at.rest) >= p.max_parts) at.s = -1;  // row ranges that overlap can make more than there is room for
             at.r.row0 = lane_value(r.row0, f);
             at.r.rows = lane_value(r.rows, f);
             at.r.held = lane_value(r.held, f);
@@ -188,7 +188,7 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
             return at;
         }
         before = sum(before, total(end));
-        at.first_item = sum(at.first_item, total(item_end));
+        at.first_part = sum(at.first_part, total(part_end));
     }
     return at;
 }

@@ -76,7 +76,7 @@ __global__ __launch_bounds__(NW * 64, PT == 1 ? 3 : 2) void attn_kv4_kernel(Kv4A
     const Request r = at.r;
     int32_t tile, split;
     const int32_t g = divide(divide(at.rest, at.tiles, tile), at.splits, split);
-    const int32_t item = at.first_item + at.rest;
+    const int32_t part = at.first_part + at.rest;
     const int32_t head0 = first_head(p, g), G = heads_of(p, g);
     const int32_t pair0 = tile * PAIRS, n_pairs_all = r.rows * G;
     const int32_t n_pairs = n_pairs_all - pair0 < PAIRS ? n_pairs_all - pair0 : PAIRS;
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(NW * 64, PT == 1 ? 3 : 2) void attn_kv4_kernel(Kv4A
                 acc += f * *reinterpret_cast<const f32x4 *>(all_o + (w * 16 + at_o) * D + d4);
             }
             if (at.splits > 1) {
-                store_part<D>(p, (int64_t)item * p.tile_pairs + pr, d4, acc, M, l);
+                store_part<D>(p, (int64_t)part * p.tile_pairs + pr, d4, acc, M, l);
             } else {
                 int32_t hh;
                 const int32_t rr = divide(pair0 + pr, G, hh);
@@ -410,11 +410,11 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void merge_kv4_kernel(Kv4
     const int32_t head0 = first_head(p, g), G = heads_of(p, g);
     const int32_t pair0 = tile << p.tile_shift, n_pairs = min(at.r.rows * G - pair0, 1 << p.tile_shift);
     if (pr * PAIRS >= n_pairs) return;
-    const int64_t item0 = at.first_item + ((int64_t)g * at.splits) * at.tiles + tile;
-    if (item0 + (int64_t)(at.splits - 1) * at.tiles >= p.max_items) return;
+    const int64_t part0 = at.first_part + ((int64_t)g * at.splits) * at.tiles + tile;
+    if (part0 + (int64_t)(at.splits - 1) * at.tiles >= p.max_parts) return;
     const int32_t mine = __builtin_amdgcn_readfirstlane(threadIdx.x / (WAVES * 64)), tid = threadIdx.x % (WAVES * 64);
     const int32_t in_tile = pr * PAIRS + mine, pair = pair0 + in_tile;
-    const int64_t slot0 = item0 * p.tile_pairs + (in_tile < p.tile_pairs ? in_tile : p.tile_pairs - 1), stride = (int64_t)at.tiles * p.tile_pairs;
+    const int64_t slot0 = part0 * p.tile_pairs + (in_tile < p.tile_pairs ? in_tile : p.tile_pairs - 1), stride = (int64_t)at.tiles * p.tile_pairs;
     const int32_t sub = tid / LPR, d4 = tid % LPR * 4;
     float M = -INFINITY, l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};

@@ -141,7 +141,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_rows_kernel(Kv4Attn p)
     const Request r = at.r;
     int32_t tile, split;
     const int32_t g = divide(divide(at.rest, at.tiles, tile), at.splits, split);
-    const int32_t item = at.first_item + at.rest;
+    const int32_t part = at.first_part + at.rest;
     const int32_t head0 = first_head(p, g), G = heads_of(p, g);
     const int32_t pair0 = tile * kPairs, n_pairs = min(r.rows * G - pair0, kPairs);
     if (n_pairs <= 0) return;
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv4_rows_kernel(Kv4Attn p)
     // ---- the lane's pair: elements b * 32 + i4 * 8 + g32 * 4 .. + 4
     const float l = l_run + __shfl_xor(l_run, 32);
     if (wave * 32 + l32 >= n_pairs) return;
-    const int64_t slot = (int64_t)item * p.tile_pairs + wave * 32 + l32;
+    const int64_t slot = (int64_t)part * p.tile_pairs + wave * 32 + l32;
 #pragma unroll
     for (int b = 0; b < DBLK; ++b)
 #pragma unroll

@@ -79,7 +79,7 @@ struct Kv4Attn {
     float *lse;
     Kv4Pool pool;
     const int32_t *table, *row_start, *row_len, *seq_len, *sink_len, *window;
-    float *part_acc, *part_ml;        // [item][tile_pairs][D], [item][tile_pairs][2]: of items that are not whole units
+    float *part_acc, *part_ml;        // [part][tile_pairs][D], [part][tile_pairs][2]: the items of units that are cut, in their order
     int32_t num_seqs, max_pages, num_rows, n_q_heads;
     int32_t tile_shift, step_shift;   // pairs of a tile, records of a step
     int32_t tile_pairs;               // pairs that a tile can have: all of a tile, or all that the rows make
@@ -88,6 +88,7 @@ struct Kv4Attn {
     int32_t shared;                   // whether there may be several tiles of the same keys
     int32_t target, min_steps;        // items that a call is cut into, if they are not shorter than this
     int32_t max_items, max_units;     // bounds that no lengths pass
+    int32_t max_parts;                // likewise, for which the workspace has room
     int32_t grid;                     // and one for the items that the table's width allows
     int32_t merge_waves, merge_grid;  // of the kernel that joins items: wavefronts of a pair, workgroups (0: no unit is cut)
     float c_log2;                     // softmax scale * log2(e)
