@@ -383,7 +383,7 @@ pevlm_status pevlm_cache_load_kv4(void *k, void *v, int64_t k_stride, int64_t v_
  * [num_rows][Hq][D], contiguous; lse: fp32 [num_rows][Hq] or NULL).  A row at position p sees token j iff
  *     j <= p  and  ( window[s] < 0  or  p - j < window[s]  or  j < sink_len[s] )
  * (window NULL: all of them; sink_len NULL: 0): a sliding window and first tokens that stay visible.  Tokens on a page outside
- * the pool are not seen.  A row that sees nothing gets zeros, and -inf in lse.  Rows of no request are left as they were, and so are those of a
+ * the pool are not seen.  A row that sees nothing, or only tokens with a score of -inf, gets zeros, and -inf in lse.  Rows of no request are left as they were, and so are those of a
  * request whose rows do not lie within [0, num_rows).  seq_len is taken within [0, max_pages * page_size].  Table entries of
  * pages without a visible token do not matter.  Several requests may name the same pages, no two the same rows.
  *

@@ -7,8 +7,8 @@
 // of two records are its share of the B operand of O^T += V^T P^T.  V comes by the same load, goes as bf16 through a slice of LDS of
 // the wavefront's own and back transposed (ds_read_b64_tr_b16).
 //
-// Roundings: Q of fp32 tensors is split into three bf16 parts that add up to it, weights into two (bf16 tensors, 2^-16) or three
-// parts (fp32); products of parts are exact in fp32, sums are fp32 throughout.  (Weights of one part save 2 %: 101 -> 99 us for 16 requests of 65.9 K
+// Roundings: Q of fp32 tensors is cut into three bf16 parts that add up to it (of numbers below 2^-103 what lies under 2^-126 is lost), weights are split into
+// two (bf16 tensors, 2^-16) or three parts (fp32); products of parts are exact in fp32, sums are fp32 throughout.  (Weights of one part save 2 %: 101 -> 99 us for 16 requests of 65.9 K
 // tokens.)
 //
 // A workgroup of four wavefronts takes an item, a run of steps of 32 tokens, the wavefronts in turn; what they have is joined in LDS.  Bound by HBM
@@ -36,6 +36,23 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&part)[N]
             a -= __uint_as_float(part[i] << 16);
             b -= __uint_as_float(part[i] & 0xffff0000u);
         }
+    }
+}
+
+// The same with parts cut off instead of rounded, 8 bits each: three hold all 24, numbers above bf16's largest stay finite (rounded, the first part would
+// be an infinity and the second its negative), and an infinity is its own first part.
+template <int N>
+__device__ __forceinline__ void cut_pair(float a, float b, uint32_t (&part)[N])
+{
+    const auto rest = [](float x) {
+        const float top = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+        return top == x ? 0.f : x - top;
+    };
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        part[i] = __float_as_uint(a) >> 16 | (__float_as_uint(b) & 0xffff0000u);
+        a = rest(a);
+        b = rest(b);
     }
 }
 
@@ -182,7 +199,7 @@ __global__ __launch_bounds__(NW * 64, PT == 1 ? 3 : 2) void attn_kv4_kernel(Kv4A
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         uint32_t part[NQ];
-                        split_pair<NQ>(q[2 * i], q[2 * i + 1], part);
+                        cut_pair<NQ>(q[2 * i], q[2 * i + 1], part);
                         for (int n = 0; n < NQ; ++n) w[n][i] = part[n];
                     }
                     for (int n = 0; n < NQ; ++n) {
