@@ -358,6 +358,9 @@ size_t pevlm_cache_pool_bytes(const pevlm_heads *heads, int32_t num_pages, int32
  * if the list does not hold the pages that it and those of the requests before it need that fit otherwise.
  * num_free is taken within [0, free_capacity], seq_len from 0 on.  num_rows: at most 2^30.  Workspace:
  * pevlm_cache_slots_workspace_bytes.
+ *
+ * The call takes pages and gives none back.  When a request ends, the caller writes its pages (the first ceil(seq_len / page_size) entries of its row
+ * of the table) behind the list's last entry, raises num_free by their number and sets seq_len to 0, on the calls' stream before the next of them.
  */
 size_t pevlm_cache_slots_workspace_bytes(int32_t num_seqs);
 pevlm_status pevlm_cache_slots(const pevlm_cache *cache, const int32_t *seq_len, const int32_t *new_len, const int32_t *free_pages,
@@ -386,6 +389,11 @@ pevlm_status pevlm_cache_load_kv4(void *k, void *v, int64_t k_stride, int64_t v_
  * the pool are not seen.  A row that sees nothing, or only tokens with a score of -inf, gets zeros, and -inf in lse.  Rows of no request are left as they were, and so are those of a
  * request whose rows do not lie within [0, num_rows).  seq_len is taken within [0, max_pages * page_size].  Table entries of
  * pages without a visible token do not matter.  Several requests may name the same pages, no two the same rows.
+ *
+ * Scores, maxima and sums are fp32.  Weights are kept to 2^-24 for fp32 tensors and to 2^-16 for bf16 ones, where they multiply the values; but to 2^-8, as
+ * in the prefill calls, where a bf16 call has many rows: max_pages * page_size is 4096 or more, and the requests ask with 65 pairs of a row and
+ * a query head of one KV head or more on average (head_dim 64: 113, and then by how full tiles of 128 pairs are).  Their sum is taken before that
+ * rounding, so lse has none of it.  Of numbers in an fp32 q below 2^-103 what lies under 2^-126 may be lost.
  *
  * The keys of a request are split over workgroups, and the parts merged, by the lengths of all requests: results are the same
  * for the same arguments, not for a request in another batch.  More than about 2^25 (row, query head) pairs are refused

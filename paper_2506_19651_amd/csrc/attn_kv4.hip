@@ -7,15 +7,16 @@
 // of two records are its share of the B operand of O^T += V^T P^T.  V comes by the same load, goes as bf16 through a slice of LDS of
 // the wavefront's own and back transposed (ds_read_b64_tr_b16).
 //
-// Roundings: Q of fp32 tensors is cut into three bf16 parts that add up to it (of numbers below 2^-103 what lies under 2^-126 is lost), weights are split into
+// Roundings: Q of fp32 tensors is cut into three bf16 parts that add up to it (of numbers below 2^-103 what lies under 2^-126 may be lost), weights are split into
 // two (bf16 tensors, 2^-16) or three parts (fp32); products of parts are exact in fp32, sums are fp32 throughout.  (Weights of one part save 2 %: 101 -> 99 us for 16 requests of 65.9 K
 // tokens.)
 //
 // A workgroup of four wavefronts takes an item, a run of steps of 32 tokens, the wavefronts in turn; what they have is joined in LDS.  Bound by HBM
 // where there are many items: 16 requests of 65.9 K tokens x 28/4 heads x 128 (577 MB) 98 us, 5.9 TB/s with both launches, 6.3 inside the kernel;
 // with all codes in the caches its arithmetic takes 60 of them (vector instructions issue 61 %, matrix cores are busy 27 % of the time).  One request of 65.9 K tokens
-// (36 MB) is a chain of round trips, 18.7 us: fields, lengths, table, records (3 us), three steps (5), the join (1), launch and merge (9).  Three
-// workgroups a compute unit are enough (four 101.6 against 100.9 us, two 111), and two steps ahead are no faster than one.
+// (36 MB) is a chain of round trips, 19.8 us with stamps in it: place (1.1), records and queries (1.7), three steps (6.2), the join (1.3), the last workgroup's
+// lag (1.7), from there to the merge's start (1.9), the merge (4.4), and from its end to the next call's start (1.5).  Three workgroups a compute unit are
+// enough (four 101.6 against 100.9 us, two 111), and two steps ahead are no faster than one.
 #include "attn_kv4.h"
 
 namespace pevlm {
@@ -408,7 +409,7 @@ __global__ __launch_bounds__(NW * 64, PT == 1 ? 3 : 2) void attn_kv4_kernel(Kv4A
 
 // Joins the items of the units that were cut.  WAVES wavefronts take a pair, a workgroup one (16) or two (2) pairs of a unit: D / 4 lanes cover a row of
 // values and the groups of them take the items in turn, kTurn at once with their maxima and sums, against a running maximum of their own; then
-// the groups are joined.  Bound by latency, 4 to 5 us: the lengths, then the parts, in one memory round trip each.  (Lanes that walk all items take a
+// the groups are joined.  Bound by latency, 4 to 6 us: the lengths, then the parts, in one memory round trip each.  (Lanes that walk all items take a
 // trip for each, 23 us for 128 items of 28 pairs, and to fetch all maxima before the first values is one trip more.)
 constexpr int kTurn = 6;
 
@@ -522,6 +523,10 @@ static void launch(const Kv4Attn &p, hipStream_t stream)
     else hipLaunchKernelGGL((merge_kv4_kernel<D, BF16, 16, FEW>), dim3(p.merge_grid), dim3(1024), 0, stream, p);
 }
 
+// Up to 64 requests the lanes hold all lengths, which are read once, and the items' length is chosen among three.  With / without, 1 row of 28/4 heads x
+// 128: 64 requests of 200 tokens 15.9 / 17.4 us, of 1000 24.2 / 25.3, of 16 K 106 / 120; 24 ragged ones of 32/8 heads 58.0 / 61.3; 4 rows of 64
+// ragged ones 132 / 168; 100 rows of 8 240 / 263.  Without, every wavefront reads the lengths of 64 requests at a time, two or three times: 65 requests of
+// 1000 tokens 27.3 us, 256 85, 1024 835.
 template <int D, bool BF16>
 static void launch(const Kv4Attn &p, hipStream_t stream)
 {

@@ -10,6 +10,8 @@ namespace pevlm {
 // at 2^32 - 1, which is more than any bound they are held to.  A step's few rows are filled in by the same workgroup from LDS; a prompt's by
 // a launch of one row a lane.  Bound by latency: 2.9 us for 64 requests of one token, 2.8 and 4.1 for four prompts of 141 K tokens.
 // ------------------------------------------------------------------------------------------
+// One launch against two, by the call: 64 requests of 1, 8 and 32 tokens 8.3 to 8.6 / 11.3 us, 1024 of one 8.6 / 11.4.  (Up to 8192 rows it would still
+// serve, four requests of 2048 tokens 8.5 / 11.4.)  Beyond 1024 requests their lengths would not stay in LDS.
 constexpr int32_t kSmallRows = 2048, kSmallRequests = 1024;
 
 // inclusive sum over the workgroup; `waves` holds the wavefronts' sums
@@ -141,6 +143,7 @@ __global__ __launch_bounds__(256) void kv4_slots_kernel(Kv4Slots p)
 hipError_t launch_kv4_slots(const Kv4Slots &p, hipStream_t stream)
 {
     if (p.num_rows <= kSmallRows && p.num_seqs <= kSmallRequests) {
+        // 256 / 1024 threads, the kernel: 64 requests of 1 token 3.0 / 3.5 us, of 8 4.4 / 4.0, of 32 10.1 / 6.0; 256 of 1 3.3 / 3.6; 512 of 1 5.4 / 4.0
         const bool few = p.num_seqs <= 256 && p.num_rows <= 512;
         if (few) hipLaunchKernelGGL((kv4_requests_kernel<256, true>), dim3(1), dim3(256), 0, stream, p);
         else hipLaunchKernelGGL((kv4_requests_kernel<1024, true>), dim3(1), dim3(1024), 0, stream, p);
