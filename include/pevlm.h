@@ -360,7 +360,8 @@ size_t pevlm_cache_pool_bytes(const pevlm_heads *heads, int32_t num_pages, int32
  * pevlm_cache_slots_workspace_bytes.
  *
  * The call takes pages and gives none back.  When a request ends, the caller writes its pages (the first ceil(seq_len / page_size) entries of its row
- * of the table) behind the list's last entry, raises num_free by their number and sets seq_len to 0, on the calls' stream before the next of them.
+ * of the table) behind the list's last entry, raises num_free by their number and sets seq_len to 0, on the calls' stream before the next of them; a
+ * request that has ended gets a new_len of 0 until its place is given to another.
  */
 size_t pevlm_cache_slots_workspace_bytes(int32_t num_seqs);
 pevlm_status pevlm_cache_slots(const pevlm_cache *cache, const int32_t *seq_len, const int32_t *new_len, const int32_t *free_pages,
@@ -386,9 +387,9 @@ pevlm_status pevlm_cache_load_kv4(void *k, void *v, int64_t k_stride, int64_t v_
  * [num_rows][Hq][D], contiguous; lse: fp32 [num_rows][Hq] or NULL).  A row at position p sees token j iff
  *     j <= p  and  ( window[s] < 0  or  p - j < window[s]  or  j < sink_len[s] )
  * (window NULL: all of them; sink_len NULL: 0): a sliding window and first tokens that stay visible.  Tokens on a page outside
- * the pool are not seen.  A row that sees nothing, or only tokens with a score of -inf, gets zeros, and -inf in lse.  Rows of no request are left as they were, and so are those of a
- * request whose rows do not lie within [0, num_rows).  seq_len is taken within [0, max_pages * page_size].  Table entries of
- * pages without a visible token do not matter.  Several requests may name the same pages, no two the same rows.
+ * the pool are not seen.  A row that sees nothing, or only tokens with a score of -inf, gets zeros, and -inf in lse.  Rows of no
+ * request are left as they were, and so are those of a request whose rows do not lie within [0, num_rows).  seq_len is taken within
+ * [0, max_pages * page_size].  Table entries of pages without a visible token do not matter.  Several requests may name the same pages, no two the same rows.
  *
  * Scores, maxima and sums are fp32.  Weights are kept to 2^-24 for fp32 tensors and to 2^-16 for bf16 ones, where they multiply the values; but to 2^-8, as
  * in the prefill calls, where a bf16 call has many rows: max_pages * page_size is 4096 or more, and the requests ask with 65 pairs of a row and

@@ -179,7 +179,8 @@ __device__ __forceinline__ Place find_place(const Kv4Attn &p, int32_t idx)
             at.splits = lane_value(splits, f);
             at.tiles = lane_value(tiles, f);
             at.first_part = sum(at.first_part, lane_value(part_end, f) - lane_value(parts, f));
-            if (!UNITS && at.splits > 1 && sum(at.first_part, at.rest) >= p.max_parts) at.s = -1;  // row ranges that overlap can make more than there is room for
+            // row ranges that overlap can make more parts than there is room for
+            if (!UNITS && at.splits > 1 && sum(at.first_part, at.rest) >= p.max_parts) at.s = -1;
             at.r.row0 = lane_value(r.row0, f);
             at.r.rows = lane_value(r.rows, f);
             at.r.held = lane_value(r.held, f);

@@ -7,9 +7,9 @@
 // of two records are its share of the B operand of O^T += V^T P^T.  V comes by the same load, goes as bf16 through a slice of LDS of
 // the wavefront's own and back transposed (ds_read_b64_tr_b16).
 //
-// Roundings: Q of fp32 tensors is cut into three bf16 parts that add up to it (of numbers below 2^-103 what lies under 2^-126 may be lost), weights are split into
-// two (bf16 tensors, 2^-16) or three parts (fp32); products of parts are exact in fp32, sums are fp32 throughout.  (Weights of one part save 2 %: 101 -> 99 us for 16 requests of 65.9 K
-// tokens.)
+// Roundings: Q of fp32 tensors is cut into three bf16 parts that add up to it (of numbers below 2^-103 what lies under 2^-126 may be
+// lost), weights are split into two (bf16 tensors, 2^-16) or three parts (fp32); products of parts are exact in fp32, sums are fp32
+// throughout.  (Weights of one part save 2 %: 101 -> 99 us for 16 requests of 65.9 K tokens.)
 //
 // A workgroup of four wavefronts takes an item, a run of steps of 32 tokens, the wavefronts in turn; what they have is joined in LDS.  Bound by HBM
 // where there are many items: 16 requests of 65.9 K tokens x 28/4 heads x 128 (577 MB) 98 us, 5.9 TB/s with both launches, 6.3 inside the kernel;
